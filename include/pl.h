@@ -398,6 +398,59 @@ int pl_sample_static(const float *logits, int32_t n, int32_t vocab, const uint64
 int pl_is_ess(const float *logp_pi, const float *logp_mu, const int64_t *seq_offsets, int32_t n_seq, float c,
               float *w_out, double *seq_sums, double *ess_seq, double *totals, void *stream);
 
+/* Log-probabilities of given tokens under an LM head (the learner's log pi of recorded tokens, to set against the behaviour
+ * log-prob in pl_is_ess), without logits in memory: with z[t, v] = inv_temperature[t] * sum_k h[t, k] w[v, k],
+ *   lse[t] = log sum_v exp z[t, v],   logprob[t] = z[t, target[t]] - lse[t]    (the distribution that pl_sample records).
+ *   h       device bf16, n rows of d hidden states (behind the final norm), ldh elements apart
+ *   w       device bf16, vocab rows of d weights, ldw elements apart: row-major, as a trainer (and a tied embedding table) has them
+ *   target  device int32 [n].  A value outside [0, vocab) means a position without a target (prompts, padding): its logprob and lse are
+ *           0, and whatever its row of h holds (NaN included) reaches no other result.  Such positions cost nothing.
+ *   inv_temperature  device fp32 [n], or NULL: 1
+ *   logprob, lse     device fp32 [n] out
+ *   workspace        device, at least pl_token_logprob_workspace_bytes(n, vocab, d) bytes, nothing of value in it afterwards
+ * bf16 products, fp32 sums.  A position's results do not depend on the other positions of the call, to the last bit.
+ * PL_E_INVAL (nothing launched; the workspace size is then 0) for n or vocab below 1 or beyond 2^24, d not a multiple of 256 or beyond
+ * 65536, a stride below d or not a multiple of 8 (ldw: beyond 2^20), h or w not aligned to 16 bytes.
+ * Asynchronous on `stream`, which belongs to the current device, as do all buffers; calls that overlap need workspaces of their own.  May be
+ * captured into a graph. */
+int64_t pl_token_logprob_workspace_bytes(int32_t n, int32_t vocab, int32_t d);
+int pl_token_logprob(const void *h, int64_t ldh, const void *w, int64_t ldw, const int32_t *target, const float *inv_temperature,
+                     float *logprob, float *lse, int32_t n, int32_t vocab, int32_t d, void *workspace, void *stream);
+
+/* Its gradient.  For a loss L with g[t] = dL/dlogprob[t], and G[t, v] = g[t] inv_temperature[t] ((v == target[t]) - exp(z[t, v] - lse[t])):
+ *   dh = G w   device bf16 [n, d], or NULL (not wanted); rows of positions without a target are 0
+ *   dw = G^T h device bf16 [vocab, d], or NULL; every row is written
+ * lse and the first six arguments are those of the forward call (lse device fp32 [n], g device fp32 [n]; neither is read where there is no
+ * target).  The logits are computed again, piece by piece of the vocabulary; G is rounded to bf16 for the products (half a step, as the
+ * operands are), sums are fp32, results are rounded once.  Results are the same bits from call to call.
+ * PL_E_INVAL as above, and for n * d * 2 bytes of 2 GiB or more, dh or dw not aligned to 16 bytes, neither asked for. */
+int64_t pl_token_logprob_grad_workspace_bytes(int32_t n, int32_t vocab, int32_t d);
+int pl_token_logprob_grad(const void *h, int64_t ldh, const void *w, int64_t ldw, const int32_t *target, const float *inv_temperature,
+                          const float *lse, const float *g, void *dh, void *dw, int32_t n, int32_t vocab, int32_t d, void *workspace,
+                          void *stream);
+
+/* Weights for pl_gemm_int8: per row (output channel) of w, device [N, K] of dtype PL_BF16 or PL_F32, rows ldw elements apart,
+ *   w_scale[n] = fl32(max_k |w[n, k]| / 127),  code = the integer nearest to w[n, k] / w_scale[n] (the exact quotient; ties to even)
+ * clamped to [-127, 127]; a scale of 0 has codes 0, a row that holds an infinity or a NaN has codes 0 and scale NaN.
+ *   w_q      device int8 [N * K] out, in operand order: blocks of 32 rows x 128 k, stored k-block by k-block (K / 128 planes of N / 32
+ *            blocks); inside a block, code (r, k) lies at ((k / 16 % 4) * 64 + (k / 64) * 32 + r) * 16 + k % 16
+ *   w_scale  device fp32 [N] out
+ * N a multiple of 32, K a multiple of 256 up to 133120, N * K below 2 GiB, rows on 16-byte boundaries (PL_E_INVAL otherwise, nothing
+ * launched).  Asynchronous on `stream` of the current device. */
+int pl_quantize_int8(const void *w, int32_t dtype, int64_t ldw, void *w_q, float *w_scale, int32_t N, int32_t K, void *stream);
+
+/* y = x W^T in 8-bit integers.  x device bf16, M rows of K, ldx elements apart, quantised row by row (per token) in the call by the same rule;
+ * w_q, w_scale from pl_quantize_int8.  With the codes xq, wq and the exact integer sum s = sum_k xq[m, k] wq[n, k]:
+ *   y[m, n] = (float(s) * x_scale[m]) * w_scale[n], device [M, N] of y_dtype PL_F32 or PL_BF16 (rounded once more).
+ * A row's results do not depend on the other rows of the call.  A row of x that holds an infinity or a NaN gives a row of NaN.
+ * workspace: device, at least pl_gemm_int8_workspace_bytes(M, N, K) bytes, nothing of value in it afterwards; calls that overlap need
+ * workspaces of their own.  PL_E_INVAL (nothing launched; the workspace size is then 0) for M < 1, N and K as above, M * K of 2 GiB or more,
+ * ldx below K or not a multiple of 8, x, w_q or y not aligned to 16 bytes.  Asynchronous on `stream` of the current device; may be
+ * captured into a graph. */
+int64_t pl_gemm_int8_workspace_bytes(int32_t M, int32_t N, int32_t K);
+int pl_gemm_int8(const void *x, int64_t ldx, const void *w_q, const float *w_scale, void *y, int32_t y_dtype, int32_t M, int32_t N, int32_t K,
+                 void *workspace, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -10,7 +10,8 @@ __all__ = [
     "PL_OK", "PL_E_INVAL", "PL_E_NOSLOT", "PL_E_NOKV", "PL_E_BUSY", "PL_E_STATE", "PL_E_CTX", "PL_E_HIP",
     "PL_E_NOMEM", "PL_SWAP_ASYNC", "PL_SWAP_WAIT", "PL_SWAP_RECOMPUTE_KV", "PL_DEVICE_NONE", "PL_BF16", "PL_F32", "PL_GEMM_COLD", "PlError", "ModelCfg", "StepOut", "Stats",
     "lib", "library_path", "Engine", "operand_order", "pl_attention_decode", "pl_attention_workspace_bytes", "pl_kv_pack_host",
-    "pl_gemm_bf16", "pl_debug_gemm_cfg", "pl_debug_gemm_plan", "pl_debug_gemm_planned", "pl_debug_gemm_folded", "pl_sample", "pl_sample_static", "pl_sample_workspace_bytes", "pl_debug_stream_read", "pl_is_ess", "EXPORTS",
+    "pl_gemm_bf16", "pl_debug_gemm_cfg", "pl_debug_gemm_plan", "pl_debug_gemm_planned", "pl_debug_gemm_folded", "pl_sample", "pl_sample_static", "pl_sample_workspace_bytes", "pl_debug_stream_read", "pl_is_ess",
+    "pl_token_logprob_workspace_bytes", "pl_token_logprob", "pl_token_logprob_grad_workspace_bytes", "pl_token_logprob_grad", "pl_quantize_int8", "pl_gemm_int8_workspace_bytes", "pl_gemm_int8", "EXPORTS",
 ]
 
 PL_OK, PL_E_INVAL, PL_E_NOSLOT, PL_E_NOKV, PL_E_BUSY, PL_E_STATE, PL_E_CTX, PL_E_HIP, PL_E_NOMEM = 0, -1, -2, -3, -4, -5, -6, -7, -8
@@ -26,6 +27,7 @@ EXPORTS = [
     "pl_num_active", "pl_decode_step", "pl_get_stats", "pl_debug_get_logits", "pl_debug_read_kv",
     "pl_debug_write_kv", "pl_debug_add_sequence_at", "pl_debug_set_history", "pl_debug_set_poison", "pl_debug_set_graphs", "pl_debug_kv_pool", "pl_debug_set_profile", "pl_debug_gemm_cfg", "pl_debug_gemm_plan", "pl_debug_gemm_planned", "pl_debug_gemm_folded", "pl_debug_stream_read", "pl_attention_workspace_bytes",
     "pl_attention_decode", "pl_kv_pack_host", "pl_gemm_bf16", "pl_sample_workspace_bytes", "pl_sample", "pl_sample_static", "pl_is_ess",
+    "pl_token_logprob_workspace_bytes", "pl_token_logprob", "pl_token_logprob_grad_workspace_bytes", "pl_token_logprob_grad", "pl_quantize_int8", "pl_gemm_int8_workspace_bytes", "pl_gemm_int8",
 ]
 
 
@@ -123,6 +125,13 @@ def lib():
         "pl_sample": (C.c_int, [vp, i32, i32, vp, vp, vp, vp, u64, vp, vp, vp, vp]),
         "pl_sample_static": (C.c_int, [vp, i32, i32, vp, vp, vp, vp, u64, vp, vp, vp]),
         "pl_is_ess": (C.c_int, [vp, vp, vp, i32, f32, vp, vp, vp, vp, vp]),
+        "pl_token_logprob_workspace_bytes": (i64, [i32, i32, i32]),
+        "pl_token_logprob": (C.c_int, [vp, i64, vp, i64, vp, vp, vp, vp, i32, i32, i32, vp, vp]),
+        "pl_token_logprob_grad_workspace_bytes": (i64, [i32, i32, i32]),
+        "pl_token_logprob_grad": (C.c_int, [vp, i64, vp, i64, vp, vp, vp, vp, vp, vp, i32, i32, i32, vp, vp]),
+        "pl_quantize_int8": (C.c_int, [vp, i32, i64, vp, vp, i32, i32, vp]),
+        "pl_gemm_int8_workspace_bytes": (i64, [i32, i32, i32]),
+        "pl_gemm_int8": (C.c_int, [vp, i64, vp, vp, vp, i32, i32, i32, i32, vp, vp]),
     }
     for name, (res, args) in sigs.items():
         fn = getattr(L, name)
@@ -433,3 +442,33 @@ def pl_sample_static(logits, n, vocab, seq_id, position, inv_temperature, forced
 def pl_is_ess(logp_pi, logp_mu, seq_offsets, n_seq, c, w_out, seq_sums, ess_seq, totals, stream=0):
     """Device pointers (ints); see include/pl.h."""
     _check(lib().pl_is_ess(logp_pi, logp_mu, seq_offsets, n_seq, c, w_out, seq_sums, ess_seq, totals, stream))
+
+
+def pl_token_logprob_workspace_bytes(n, vocab, d):
+    return int(lib().pl_token_logprob_workspace_bytes(n, vocab, d))
+
+
+def pl_token_logprob(h, ldh, w, ldw, target, inv_temperature, logprob, lse, n, vocab, d, workspace, stream=0):
+    """Device pointers (ints; inv_temperature may be 0); see include/pl.h."""
+    _check(lib().pl_token_logprob(h, ldh, w, ldw, target, inv_temperature, logprob, lse, n, vocab, d, workspace, stream))
+
+
+def pl_token_logprob_grad_workspace_bytes(n, vocab, d):
+    return int(lib().pl_token_logprob_grad_workspace_bytes(n, vocab, d))
+
+
+def pl_token_logprob_grad(h, ldh, w, ldw, target, inv_temperature, lse, g, dh, dw, n, vocab, d, workspace, stream=0):
+    """Device pointers (ints; inv_temperature, and dh or dw, may be 0); see include/pl.h."""
+    _check(lib().pl_token_logprob_grad(h, ldh, w, ldw, target, inv_temperature, lse, g, dh, dw, n, vocab, d, workspace, stream))
+
+
+def pl_quantize_int8(w, dtype, ldw, w_q, w_scale, N, K, stream=0):
+    _check(lib().pl_quantize_int8(w, dtype, ldw, w_q, w_scale, N, K, stream))
+
+
+def pl_gemm_int8_workspace_bytes(M, N, K):
+    return int(lib().pl_gemm_int8_workspace_bytes(M, N, K))
+
+
+def pl_gemm_int8(x, ldx, w_q, w_scale, y, y_dtype, M, N, K, workspace, stream=0):
+    _check(lib().pl_gemm_int8(x, ldx, w_q, w_scale, y, y_dtype, M, N, K, workspace, stream))

@@ -271,4 +271,23 @@ int launch_tie_lm_head(const void *embed, void *lm_head, int vocab, int d, bool 
 int launch_is_ess(const float *lp_pi, const float *lp_mu, const int64_t *offsets, int n_seq, double c, float *w_out,
                   double *seq_sums, double *ess_seq, double *totals, hipStream_t s);
 
+// positions of packed sequences, their targets and the LM head (kernels_loss.hip)
+struct TokenLoss {
+  const bf16_t *h; int64_t ldh;
+  const bf16_t *w; int64_t ldw;
+  const int32_t *target;
+  const float *inv_t;       // or null: 1
+  int32_t n, vocab, d;
+  void *workspace;          // on a boundary of 256 bytes
+};
+int64_t token_logprob_workspace_bytes(int n, int vocab, int d);
+int launch_token_logprob(const TokenLoss &p, float *logprob, float *lse, hipStream_t s);
+int64_t token_logprob_grad_workspace_bytes(int n, int vocab, int d);
+int launch_token_logprob_grad(const TokenLoss &p, const float *lse, const float *g, bf16_t *dh, bf16_t *dw, hipStream_t s);
+
+// products in 8-bit integers (kernels_int8.hip)
+int launch_quantize_int8(const void *w, bool f32, int64_t ldw, int8_t *q, float *scale, int N, int K, hipStream_t s);
+int64_t gemm_int8_workspace_bytes(int M, int N, int K);
+int launch_gemm_int8(const bf16_t *x, int64_t ldx, const int8_t *wq, const float *sw, void *y, bool f32, int M, int N, int K, void *ws, hipStream_t s);
+
 }  // namespace pl

@@ -1837,4 +1837,87 @@ int pl_sample_static(const float *logits, int32_t n, int32_t vocab, const uint64
   return PL_OK;
 }
 
+// ---- token log-probabilities and 8-bit products -------------------------------------------------------
+
+static void *aligned256(void *p) { return (void *)(((uintptr_t)p + 255) & ~(uintptr_t)255); }
+static bool misaligned(const void *p) { return ((uintptr_t)p & 15) != 0; }
+
+// what both calls ask of their operands; null where it is met
+static const char *token_loss_refusal(const void *h, int64_t ldh, const void *w, int64_t ldw, int32_t n, int32_t vocab, int32_t d) {
+  if (n < 1 || vocab < 1) return "need n >= 1 and vocab >= 1";
+  if (d < 256 || d % 256 || d > 65536) return "d must be a multiple of 256, at most 65536";
+  if (ldh < d || ldw < d || ldh % 8 || ldw % 8 || ldw > (1 << 20)) return "row strides must be multiples of 8, at least d (ldw at most 2^20)";
+  if (misaligned(h) || misaligned(w)) return "h and w must be aligned to 16 bytes";
+  if (vocab > (1 << 24) || n > (1 << 24)) return "at most 2^24 positions and vocabulary rows";
+  return nullptr;
+}
+
+int64_t pl_token_logprob_workspace_bytes(int32_t n, int32_t vocab, int32_t d) {
+  if (token_loss_refusal(nullptr, d, nullptr, d, n, vocab, d)) return 0;
+  return pl::token_logprob_workspace_bytes(n, vocab, d) + 256;
+}
+
+int pl_token_logprob(const void *h, int64_t ldh, const void *w, int64_t ldw, const int32_t *target, const float *inv_temperature,
+                     float *logprob, float *lse, int32_t n, int32_t vocab, int32_t d, void *workspace, void *stream) {
+  if (!h || !w || !target || !logprob || !lse || !workspace) return fail(PL_E_INVAL, "NULL argument");
+  if (const char *why = token_loss_refusal(h, ldh, w, ldw, n, vocab, d)) return fail(PL_E_INVAL, "%s (n = %d, vocab = %d, d = %d)", why, n, vocab, d);
+  const pl::TokenLoss p{(const bf16_t *)h, ldh, (const bf16_t *)w, ldw, target, inv_temperature, n, vocab, d, aligned256(workspace)};
+  if (pl::launch_token_logprob(p, logprob, lse, (hipStream_t)stream)) return fail(PL_E_HIP, "log-probability launch failed");
+  return PL_OK;
+}
+
+// dW adds over all positions at once, and their hidden states lie behind one 32-bit offset
+static bool grad_fits(int32_t n, int32_t d) { return (int64_t)n * d * 2 < pl::GEMM_MAX_OPERAND_BYTES; }
+
+int64_t pl_token_logprob_grad_workspace_bytes(int32_t n, int32_t vocab, int32_t d) {
+  if (token_loss_refusal(nullptr, d, nullptr, d, n, vocab, d) || !grad_fits(n, d)) return 0;
+  return pl::token_logprob_grad_workspace_bytes(n, vocab, d) + 256;
+}
+
+int pl_token_logprob_grad(const void *h, int64_t ldh, const void *w, int64_t ldw, const int32_t *target, const float *inv_temperature,
+                          const float *lse, const float *g, void *dh, void *dw, int32_t n, int32_t vocab, int32_t d, void *workspace,
+                          void *stream) {
+  if (!h || !w || !target || !lse || !g || !workspace) return fail(PL_E_INVAL, "NULL argument");
+  if (!dh && !dw) return fail(PL_E_INVAL, "neither dh nor dw is asked for");
+  if (const char *why = token_loss_refusal(h, ldh, w, ldw, n, vocab, d)) return fail(PL_E_INVAL, "%s (n = %d, vocab = %d, d = %d)", why, n, vocab, d);
+  if (!grad_fits(n, d)) return fail(PL_E_INVAL, "%d positions of %d: 2 GiB of hidden states or more; split the batch", n, d);
+  if (misaligned(dh) || misaligned(dw)) return fail(PL_E_INVAL, "dh and dw must be aligned to 16 bytes");
+  const pl::TokenLoss p{(const bf16_t *)h, ldh, (const bf16_t *)w, ldw, target, inv_temperature, n, vocab, d, aligned256(workspace)};
+  if (pl::launch_token_logprob_grad(p, lse, g, (bf16_t *)dh, (bf16_t *)dw, (hipStream_t)stream)) return fail(PL_E_HIP, "gradient launch failed");
+  return PL_OK;
+}
+
+// sums of products of codes stay inside int32, operands behind 32-bit offsets
+static const char *int8_refusal(int32_t M, int32_t N, int32_t K) {
+  if (M < 1 || N < 32 || N % 32) return "need M >= 1 and N a positive multiple of 32";
+  if (K < 256 || K % 256 || (int64_t)K * 127 * 127 > INT32_MAX) return "K must be a multiple of 256, at most 133120";
+  if ((int64_t)N * K >= pl::GEMM_MAX_OPERAND_BYTES || (int64_t)M * K >= pl::GEMM_MAX_OPERAND_BYTES) return "an operand's codes must stay below 2 GiB";
+  return nullptr;
+}
+
+int pl_quantize_int8(const void *w, int32_t dtype, int64_t ldw, void *w_q, float *w_scale, int32_t N, int32_t K, void *stream) {
+  if (!w || !w_q || !w_scale) return fail(PL_E_INVAL, "NULL argument");
+  if (dtype != PL_BF16 && dtype != PL_F32) return fail(PL_E_INVAL, "dtype must be PL_BF16 or PL_F32");
+  if (const char *why = int8_refusal(1, N, K)) return fail(PL_E_INVAL, "%s (N = %d, K = %d)", why, N, K);
+  if (ldw < K || ldw % (dtype == PL_F32 ? 4 : 8) || misaligned(w) || misaligned(w_q)) return fail(PL_E_INVAL, "rows must start on 16-byte boundaries, at least K apart");
+  if (pl::launch_quantize_int8(w, dtype == PL_F32, ldw, (int8_t *)w_q, w_scale, N, K, (hipStream_t)stream)) return fail(PL_E_HIP, "quantisation launch failed");
+  return PL_OK;
+}
+
+int64_t pl_gemm_int8_workspace_bytes(int32_t M, int32_t N, int32_t K) {
+  if (int8_refusal(M, N, K)) return 0;
+  return pl::gemm_int8_workspace_bytes(M, N, K) + 256;
+}
+
+int pl_gemm_int8(const void *x, int64_t ldx, const void *w_q, const float *w_scale, void *y, int32_t y_dtype, int32_t M, int32_t N, int32_t K,
+                 void *workspace, void *stream) {
+  if (!x || !w_q || !w_scale || !y || !workspace) return fail(PL_E_INVAL, "NULL argument");
+  if (y_dtype != PL_BF16 && y_dtype != PL_F32) return fail(PL_E_INVAL, "y_dtype must be PL_BF16 or PL_F32");
+  if (const char *why = int8_refusal(M, N, K)) return fail(PL_E_INVAL, "%s (M = %d, N = %d, K = %d)", why, M, N, K);
+  if (ldx < K || ldx % 8 || misaligned(x) || misaligned(w_q) || misaligned(y)) return fail(PL_E_INVAL, "x, w_q and y must be aligned to 16 bytes, rows of x at least K apart and multiples of 8");
+  const int rc = pl::launch_gemm_int8((const bf16_t *)x, ldx, (const int8_t *)w_q, w_scale, y, y_dtype == PL_F32, M, N, K, aligned256(workspace), (hipStream_t)stream);
+  if (rc) return fail(PL_E_HIP, "int8 product launch failed");
+  return PL_OK;
+}
+
 }  // extern "C"
