@@ -1867,7 +1867,7 @@ int pl_token_logprob(const void *h, int64_t ldh, const void *w, int64_t ldw, con
 }
 
 // dW adds over all positions at once, and their hidden states lie behind one 32-bit offset
-static bool grad_fits(int32_t n, int32_t d) { return (int64_t)n * d * 2 < pl::GEMM_MAX_OPERAND_BYTES; }
+static bool grad_fits(int32_t n, int32_t d) { return ((int64_t)n + 255) / 256 * 256 * d * 2 < pl::GEMM_MAX_OPERAND_BYTES; }
 
 int64_t pl_token_logprob_grad_workspace_bytes(int32_t n, int32_t vocab, int32_t d) {
   if (token_loss_refusal(nullptr, d, nullptr, d, n, vocab, d) || !grad_fits(n, d)) return 0;
