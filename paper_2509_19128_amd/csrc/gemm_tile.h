@@ -8,6 +8,17 @@ namespace {
 constexpr int BK = 64;          // k elements per main-loop step
 constexpr int STAGES = 4;       // k-steps held: one is multiplied while three are on their way
 typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+// Of sixteen lanes with 4 x 16 values (four lanes to a row of 32 bytes), lane i gets column i.  (__restrict__: a read of LDS of which the compiler knows
+// nothing waits for every load on its way there; this one it takes for apart from them, as it does ordinary reads, whose waits are written out.)
+__device__ __forceinline__ s16x4 read_transposed(lds_s16x4 *__restrict__ p) {
+#ifdef __HIP_DEVICE_COMPILE__
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16(p);
+#else
+  return s16x4{};
+#endif
+}
 // Cache policy of the W loads: non-temporal (2) for weights that are COLD, that is, cannot be in the 256 MB last-level cache
 // from the pass before, in tiles whose W one wavefront reads (WM = 1): they have no second reader, and ordinary loads
 // evict each other from L2 on the way.  SwiGLU of the 32B shape, 128 rows: 111.8 -> 98.7 us (5.7 TB/s); 7B shape, 19 rows,
@@ -41,11 +52,14 @@ struct Tile {
   static constexpr int BM = WM * AT * 32, BN = WN * BT * 32;
   static constexpr int XI = BM / 32, XH = (XI + 1) / 2, WI = BT * 4;   // loads of a wavefront per k-step: x (half of them XH), W
   static constexpr int STAGE = BM * BK, LDS = STAGES * STAGE;          // elements
+  // Offsets of x held per lane: one per load; of the kinds that address whole tiles, those that differ by more than a number of rows, which a scalar
+  // adds (their kernels have no register to spare: a spill in the main loop waits for every load in flight).
+  static constexpr int XL = KIND < TILE_COLS ? XI : KIND == TILE_COLS ? 1 : BM == 256 ? 2 : 1;
   static_assert(WM * WN == 4 && BT <= 2, "tile");
 
   // where a tile's operands are
   struct Part {
-    int x_lane[XI];        // per lane: byte offset of its row and chunk (rows beyond M repeat the last one)
+    int x_lane[XL];        // per lane: byte offset of its row and chunk (rows beyond M repeat the last one)
     int x_k;               // byte offset of the first k
     uint32_t w_blk[BT];    // byte offset of the first W block
   };
@@ -56,7 +70,7 @@ struct Tile {
   __amdgpu_buffer_rsrc_t rw, rx;   // one resource per operand; what is uniform across a wavefront is in scalar registers
   uint32_t w_plane;
   int wave, wm, wn, l, lrow, half, a_off[4];
-  int x_step;                      // bytes from a k-step of x to the next (TILE_COLS_T)
+  int x_step, x_load;              // bytes from a k-step of x to the next, and from a wavefront's load of 64 chunks to the next (TILE_COLS and on)
   bf16_t *xs;
   typedef std::conditional_t<KIND == TILE_INT8, i32x16, f32x16> Acc;
   Acc acc[AT][BT];
@@ -102,7 +116,7 @@ struct Tile {
       }
     }
   }
-  // x: rows (TILE_COLS_T: k) ldx elements apart from X on, of which `rows` exist (TILE_COLS: further ones repeat the last; TILE_COLS_T: read as 0);
+  // x: rows (TILE_COLS_T: k) ldx elements apart from X on, of which `rows` exist (further ones read as 0);
   // w: operand-ordered, `n` of its rows per plane and `planes` k-steps from W on (further ones read as 0), the tile's from w_row on.
   __device__ __forceinline__ Part part_cols(const bf16_t *X, int64_t ldx, int rows, const bf16_t *W, int n, int planes, int w_row) {
     Part p;
@@ -110,16 +124,14 @@ struct Tile {
     rw = __builtin_amdgcn_make_buffer_rsrc((void *)W, 0, (int)((uint32_t)planes * w_plane), 0x00020000);
     const int64_t x_bytes = (int64_t)rows * ldx * 2;
     rx = __builtin_amdgcn_make_buffer_rsrc((void *)X, 0, (int)min(x_bytes, (int64_t)0x7fffffff), 0x00020000);
-    x_step = (int)(BK * 2 * ldx);
+    constexpr int PER = KIND == TILE_COLS_T ? BM / 8 : BK / 8, ROWS = 64 / PER;   // chunks of a row (of 64 k or of BM columns), rows of a load
+    static_assert(KIND != TILE_COLS_T || ROWS * XL == 4, "the slots of a row go by its number modulo 4");
+    x_step = KIND == TILE_COLS_T ? (int)(BK * 2 * ldx) : BK * 2;
+    x_load = (int)(ROWS * 2 * ldx);
 #pragma unroll
-    for (int i = 0; i < XI; ++i) {
-      if constexpr (KIND == TILE_COLS_T) {
-        constexpr int PER = BM / 8;   // chunks of a row
-        const int at = (wave * XI + i) * 64 + l, k = at / PER;
-        p.x_lane[i] = (int)(k * ldx * 2) + ((at % PER) ^ (4 * (k & 3))) * 16;
-      } else {
-        p.x_lane[i] = (int)(min((wave * XI + i) * 8 + (l >> 3), rows - 1) * ldx * 2) + ((l & 7) ^ (l >> 3)) * 16;
-      }
+    for (int i = 0; i < XL; ++i) {
+      const int k = l / PER;
+      p.x_lane[i] = (int)(k * ldx * 2) + ((l % PER) ^ (KIND == TILE_COLS_T ? 4 * ((i * ROWS + k) & 3) : l / PER)) * 16;
     }
     p.x_k = 0;
 #pragma unroll
@@ -138,8 +150,8 @@ struct Tile {
 #ifdef __HIP_DEVICE_COMPILE__
 #pragma unroll
     for (int i = i0; i < i1; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (lds_void *)(xs + st * STAGE + (wave * XI + i) * 512), 16, p.x_lane[i],
-                                               p.x_k + ks * (KIND == TILE_COLS_T ? x_step : BK * 2), 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (lds_void *)(xs + st * STAGE + (wave * XI + i) * 512), 16, p.x_lane[i % XL],
+                                               KIND < TILE_COLS ? p.x_k + ks * (BK * 2) : ks * x_step + (wave * XI + i) * x_load, 0, 0);
 #endif
   }
   __device__ __forceinline__ void load_w(const Part &p, int st, int ks, int b) {
@@ -158,11 +170,8 @@ struct Tile {
     for (int a = 0; a < AT; ++a) {
       if constexpr (KIND == TILE_COLS_T) {
 #ifdef __HIP_DEVICE_COMPILE__
-        typedef __attribute__((ext_vector_type(4))) short s16x4;
-        typedef __attribute__((ext_vector_type(8))) short s16x8;
-        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
         bf16_t *at = xs + st * STAGE + a_off[a & 3] + (a >> 2) * 128 + j * 8 * BM;
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)at), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 4 * BM));
+        const s16x4 lo = read_transposed((lds_s16x4 *)at), hi = read_transposed((lds_s16x4 *)(at + 4 * BM));
         af[j & 1][a] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 #endif
       } else {
@@ -200,6 +209,21 @@ struct Tile {
 #ifdef __HIP_DEVICE_COMPILE__
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #endif
+  }
+  // Results for kernels that compute with them: one register at a time, from where the matrix cores have them.  (As ordinary operands whole accumulators are
+  // copied, which pushes other registers out to memory.)  `settle` first: the wait states that a read behind the last product needs.
+  __device__ __forceinline__ void settle() const {
+#ifdef __HIP_DEVICE_COMPILE__
+    asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+#endif
+  }
+  __device__ __forceinline__ float result(int a, int b, int i) const {
+    float v = 0.f;
+#ifdef __HIP_DEVICE_COMPILE__
+    asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v) : "a"(acc[a][b][i]));
+#endif
+    return v;
   }
   // Issue order of a quarter of a k-step: LDS reads (for the next quarter) and VM loads one by one between the products.
   template <int VM, bool READS>

@@ -91,29 +91,43 @@ struct Item {
   int kind, row0, col0;   // of the kernel's own
 };
 
-// Tiles one after the other, the next one's first k-steps under the last products of the one at hand.  next(item): the next tile, or false;
-// `next` is called as the tile before begins and `take` when its answer is needed (both by the whole workgroup).
-template <typename T, typename Next, typename Take, typename Done>
-__device__ __forceinline__ void walk(T &t, Item c, Next next, Take take, Done done) {
+// Tiles one after the other, the next one's first k-steps under the last products of the one at hand.  take(item): the next tile, or false; a tile is
+// known one tile ahead, and ask() is called as a tile begins, in time for the take() behind it.  One loop of four k-steps for all of a tile: with last k-steps
+// of their own, behind the loop, the accumulators move between the two, and what spills meanwhile waits for every load in flight.
+template <typename T, typename Ask, typename Take, typename Done>
+__device__ __forceinline__ void walk(T &t, Ask ask, Take take, Done done) {
   auto part = [&](const Item &i) { return t.part_cols(i.x, i.ldx, i.x_rows, i.w, i.w_n, i.w_planes, i.w_row); };
+  Item c, d;
+  if (!take(c)) return;
+  d = c;   // behind the last tile: its own first k-steps again, which nothing reads
+  bool more = take(d);
   auto p = part(c);
   t.zero();
   t.begin(p);
+  ask();
   for (;;) {
-    next();
-    int ks = 0;
-    for (; ks < c.ksteps - 4; ks += 4) t.four(p, ks);
-    t.template kstep<0, true, 3>(p, ks + 3);
-    Item d = c;   // behind the last tile: its own first k-steps again, which nothing reads
-    const bool more = take(d);
-    if (more) p = part(d);
-    t.template kstep<1, true, 3>(p, 0);
-    t.template kstep<2, true, 3>(p, 1);
-    t.template kstep<3, true, 3>(p, 2);
+    for (int ks = 0; ks >= 0;) {
+      t.template kstep<0, true, 3>(p, ks + 3);
+      ks += 4;
+      int at = ks;
+      if (ks >= c.ksteps) {
+        p = part(d);
+        at = 0;
+        ks = -1;
+      }
+      t.template kstep<1, true, 3>(p, at);
+      t.template kstep<2, true, 3>(p, at + 1);
+      t.template kstep<3, true, 3>(p, at + 2);
+    }
+    // what `done` computes from the lane alone is not to be held in registers through the k-steps
+    asm volatile("" : "+v"(t.lrow), "+v"(t.half));
+    t.settle();
     done(c);
     if (!more) break;
     t.zero();
     c = d;
+    more = take(d);
+    ask();
   }
   t.drain();
 }
@@ -160,15 +174,12 @@ __global__ __launch_bounds__(256) void loss_forward_kernel(Head q, const bf16_t 
   if (tiles.at >= tiles.end) return;
   T t;
   t.init_cols(xs);
-  auto item = [&]() {
+  walk(t, [] {}, [&](Item &d) {
+    if (tiles.at >= tiles.end) return false;
     int mt, vt;
     tiles.place(mt, vt);
-    return logit_item<T>(q, op, n_pad, 0, mt, vt);
-  };
-  walk(t, item(), [] {}, [&](Item &d) {
+    d = logit_item<T>(q, op, n_pad, 0, mt, vt);
     tiles.at += gridDim.x >> 3;
-    if (tiles.at >= tiles.end) return false;
-    d = item();
     return true;
   }, [&](const Item &c) {
     const int v0 = c.col0 + t.wm * AT * 32;
@@ -183,13 +194,13 @@ __global__ __launch_bounds__(256) void loss_forward_kernel(Head q, const bf16_t 
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) z[h][i] = t.acc[a + h][b][i] * row.inv_t;
+          for (int i = 0; i < 16; ++i) z[h][i] = t.result(a + h, b, i) * row.inv_t;
         if (v + GROUP > q.vocab) {   // (uniform: the last tile's entries beyond the vocabulary)
 #pragma unroll
           for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-              if (v + h * 32 + (i >> 2) * 8 + t.half * 4 + (i & 3) >= q.vocab) z[h][i] = -INFINITY;
+              if (h * 32 + (i >> 2) * 8 + (i & 3) >= q.vocab - v - t.half * 4) z[h][i] = -INFINITY;
         }
         const int y = row.target - v;
         if (__ballot(y >= 0 && y < GROUP)) {
@@ -197,7 +208,7 @@ __global__ __launch_bounds__(256) void loss_forward_kernel(Head q, const bf16_t 
           for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-              if (y == h * 32 + (i >> 2) * 8 + t.half * 4 + (i & 3) && r < count) zt[r] = z[h][i];
+              if (y - t.half * 4 == h * 32 + (i >> 2) * 8 + (i & 3) && r < count) zt[r] = z[h][i];
         }
         float m = z[0][0];
 #pragma unroll
@@ -212,6 +223,9 @@ __global__ __launch_bounds__(256) void loss_forward_kernel(Head q, const bf16_t 
           for (int i = 0; i < 16; ++i) s += __builtin_amdgcn_exp2f((z[h][i] - m) * LOG2E);
         s = with_xor32(s, OpSum{});
         if (t.half == 0 && r < count && v < q.vocab) parts[(int64_t)(v / GROUP) * n_pad + r] = make_float2(m, s);
+#ifdef __HIP_DEVICE_COMPILE__
+        __builtin_amdgcn_sched_barrier(0);   // (one block's registers at a time)
+#endif
       }
     }
   });
@@ -297,23 +311,20 @@ __global__ __launch_bounds__(256) void loss_grad_logits_kernel(Head q, const bf1
   if (tiles.at >= tiles.end) return;
   T t;
   t.init_cols(xs);
-  bf16x8 unit[2];
-#pragma unroll
-  for (int f = 0; f < 2; ++f)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) unit[f][e] = (bf16_t)(t.lrow == f * 16 + t.half * 8 + e ? 1.f : 0.f);
-  auto item = [&]() {
+  walk(t, [] {}, [&](Item &d) {
+    if (tiles.at >= tiles.end) return false;
     int mt, vt;
     tiles.place(mt, vt);
-    return logit_item<T>(q, op, n_pad, v_begin, mt, vt);
-  };
-  walk(t, item(), [] {}, [&](Item &d) {
+    d = logit_item<T>(q, op, n_pad, v_begin, mt, vt);
     tiles.at += gridDim.x >> 3;
-    if (tiles.at >= tiles.end) return false;
-    d = item();
     return true;
   }, [&](const Item &c) {
     const int v0 = c.col0 + t.wm * AT * 32;
+    bf16x8 unit[2];
+#pragma unroll
+    for (int f = 0; f < 2; ++f)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) unit[f][e] = (bf16_t)(t.lrow - t.half * 8 == f * 16 + e ? 1.f : 0.f);
 #pragma unroll
     for (int b = 0; b < BT; ++b) {
       const int m32 = (c.row0 >> 5) + t.wn * BT + b;
@@ -323,16 +334,16 @@ __global__ __launch_bounds__(256) void loss_grad_logits_kernel(Head q, const bf1
         const int v = v0 + a * 32, v32 = (v - v_begin) >> 5, y = row.target - v;
         float G[16];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) G[i] = -row.scale * __builtin_amdgcn_exp2f((t.acc[a][b][i] * row.inv_t - row.lse) * LOG2E);
+        for (int i = 0; i < 16; ++i) G[i] = -row.scale * __builtin_amdgcn_exp2f((t.result(a, b, i) * row.inv_t - row.lse) * LOG2E);
         if (__ballot(y >= 0 && y < 32)) {
 #pragma unroll
           for (int i = 0; i < 16; ++i)
-            if (y == (i >> 2) * 8 + t.half * 4 + (i & 3)) G[i] += row.scale;
+            if (y - t.half * 4 == (i >> 2) * 8 + (i & 3)) G[i] += row.scale;
         }
         if (v + 32 > q.vocab) {
 #pragma unroll
           for (int i = 0; i < 16; ++i)
-            if (v + (i >> 2) * 8 + t.half * 4 + (i & 3) >= q.vocab) G[i] = 0.f;
+            if ((i >> 2) * 8 + (i & 3) >= q.vocab - v - t.half * 4) G[i] = 0.f;
         }
         uint4 f[2];
         fragments(f, G);
@@ -375,8 +386,10 @@ struct GradParams {
 // are the longer ones, first, from their own XCD's eighth of each kind, then from the others'.
 __global__ __launch_bounds__(256) void loss_grad_kernel(Head q, GradParams g) {
   typedef Tile<1, 4, 8, 2, false, TILE_COLS_T> T;
-  __shared__ __attribute__((aligned(1024))) bf16_t xs[T::LDS];
-  __shared__ volatile int32_t drawn[2];
+  // (one LDS object: of two the compiler would know that loads on their way to one may not be what a read of it wants, and wait for them all)
+  __shared__ __attribute__((aligned(1024))) bf16_t xs[T::LDS + 4];
+  typedef __attribute__((address_space(3))) volatile int32_t lds_int;
+  lds_int *drawn = (lds_int *)(xs + T::LDS);
   const int count = *q.count, nd = q.d / 256, nm = (count + 255) / 256, nv = (g.n_v + TILE_V - 1) / TILE_V;
   const int planes = (count + g.tile_rows - 1) / g.tile_rows * g.tile_rows / BK;      // of by_entry that exist
   const int k_all = nv * (TILE_V / BK), k_slice = g.k_slice;
@@ -410,15 +423,17 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(Head q, GradParams g) {
     }
     return c;
   };
-  if (threadIdx.x == 0) drawn[1] = draw();
+  if (threadIdx.x == 0) {
+    drawn[0] = draw();
+    drawn[1] = draw();
+  }
   __syncthreads();
-  const int i0 = __builtin_amdgcn_readfirstlane(drawn[1]);
-  if (i0 < 0) return;
+  if (drawn[0] < 0) return;
   T t;
   t.init_cols(xs);
   int turn = 0;
-  walk(t, item(i0), [&] {
-    if (threadIdx.x == 0) drawn[turn] = draw();   // (read behind the barriers of this tile's k-steps, written again two tiles on)
+  walk(t, [&] {
+    if (threadIdx.x == 0) drawn[turn] = draw();   // for the tile behind the next: its place was read a tile ago, and is read again behind this tile's barriers
   }, [&](Item &d) {
     const int i = __builtin_amdgcn_readfirstlane(drawn[turn]);
     turn ^= 1;
@@ -433,14 +448,17 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(Head q, GradParams g) {
         float *o = g.dh32 + ((int64_t)c.kind * g.n_pad + r) * q.d + c.col0 + t.half * 4;
         if (r < count) {
 #pragma unroll
-          for (int a = 0; a < 8; ++a)
+          for (int a = 0; a < 8; ++a) {
+            f32x4 sum[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              f32x4 v{t.acc[a][b][4 * i], t.acc[a][b][4 * i + 1], t.acc[a][b][4 * i + 2], t.acc[a][b][4 * i + 3]};
-              f32x4 *at = (f32x4 *)(o + a * 32 + i * 8);
-              if (g.v_begin > 0) v += *at;
-              *at = v;
-            }
+            for (int i = 0; i < 4; ++i) sum[i] = g.v_begin > 0 ? *(const f32x4 *)(o + a * 32 + i * 8) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              *(f32x4 *)(o + a * 32 + i * 8) = sum[i] + f32x4{t.result(a, b, 4 * i), t.result(a, b, 4 * i + 1), t.result(a, b, 4 * i + 2), t.result(a, b, 4 * i + 3)};
+#ifdef __HIP_DEVICE_COMPILE__
+            __builtin_amdgcn_sched_barrier(0);   // (one block's registers at a time)
+#endif
+          }
         }
       } else {
         bf16_t *o = g.dw + (int64_t)(g.v_begin + r) * q.d + c.col0 + t.half * 8;
@@ -448,13 +466,16 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(Head q, GradParams g) {
         for (int a = 0; a < 8; ++a) {
           float v[16];
 #pragma unroll
-          for (int i = 0; i < 16; ++i) v[i] = t.acc[a][b][i];
+          for (int i = 0; i < 16; ++i) v[i] = t.result(a, b, i);
           uint4 f[2];
           fragments(f, v);
           if (g.v_begin + r < q.vocab) {
 #pragma unroll
             for (int k = 0; k < 2; ++k) *(uint4 *)(o + a * 32 + k * 16) = f[k];
           }
+#ifdef __HIP_DEVICE_COMPILE__
+          __builtin_amdgcn_sched_barrier(0);   // (one block's registers at a time)
+#endif
         }
       }
     }
