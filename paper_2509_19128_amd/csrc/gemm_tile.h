@@ -41,7 +41,7 @@ constexpr int W_CACHE = WM == 1 && COLD ? 2 : 0;
 // Row r of an LDS stage holds its eight 16-byte chunks at slots chunk ^ (r & 7): a direct load fills a KiB in lane order, 8 whole rows,
 // and the reads of a fragment (one chunk of 32 rows) meet every bank once.
 // The products are taken with W as the first operand: a lane ends with one row and groups of four consecutive columns.
-// Other kinds than TILE_ROWS: TILE_INT8, codes in 8 bits (a k-step is 128 of them: K counts pairs) and sums in int32;
+// Other kinds than TILE_ROWS: TILE_INT8, codes in 8 bits (a k-step is 128 of them: strides count pairs) and sums in int32;
 // TILE_COLS, x as the first operand, so that a lane ends with one column of W and groups of four consecutive rows of x;
 // TILE_COLS_T, the same with x k-major in memory (a row of it is one k): a k-step's 64 rows of BM lie in LDS as they come, and transposing reads
 // bring a lane its four k of one column, two reads per fragment.  Row k has its 16-byte chunks at slots chunk ^ 4 (k & 3), so that the four
@@ -54,7 +54,7 @@ struct Tile {
   static constexpr int STAGE = BM * BK, LDS = STAGES * STAGE;          // elements
   // Offsets of x held per lane: one per load; of the kinds that address whole tiles, those that differ by more than a number of rows, which a scalar
   // adds (their kernels have no register to spare: a spill in the main loop waits for every load in flight).
-  static constexpr int XL = KIND < TILE_COLS ? XI : KIND == TILE_COLS ? 1 : BM == 256 ? 2 : 1;
+  static constexpr int XL = KIND == TILE_ROWS ? XI : KIND != TILE_COLS_T ? 1 : BM == 256 ? 2 : 1;
   static_assert(WM * WN == 4 && BT <= 2, "tile");
 
   // where a tile's operands are
@@ -70,7 +70,7 @@ struct Tile {
   __amdgpu_buffer_rsrc_t rw, rx;   // one resource per operand; what is uniform across a wavefront is in scalar registers
   uint32_t w_plane;
   int wave, wm, wn, l, lrow, half, a_off[4];
-  int x_step, x_load;              // bytes from a k-step of x to the next, and from a wavefront's load of 64 chunks to the next (TILE_COLS and on)
+  int x_step, x_load;              // bytes from a k-step of x to the next, and from a wavefront's load of 64 chunks to the next (other kinds than TILE_ROWS)
   bf16_t *xs;
   typedef std::conditional_t<KIND == TILE_INT8, i32x16, f32x16> Acc;
   Acc acc[AT][BT];
@@ -99,8 +99,8 @@ struct Tile {
       p.w_blk[b] = (uint32_t)ks0 * w_plane + (uint32_t)min(((n_tile0 + wn * BT * 32) >> 5) + b, (N >> 5) - 1) * 4096u;
     return p;
   }
-  // The same for the kinds that take their operands tile by tile, from pointers of their own.
-  __device__ __forceinline__ void init_cols(bf16_t *xs_) {
+  // The same for the other kinds, which take their operands tile by tile, from pointers of their own.
+  __device__ __forceinline__ void init_at(bf16_t *xs_) {
     xs = xs_;
     l = threadIdx.x & 63;
     wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -118,7 +118,7 @@ struct Tile {
   }
   // x: rows (TILE_COLS_T: k) ldx elements apart from X on, of which `rows` exist (further ones read as 0);
   // w: operand-ordered, `n` of its rows per plane and `planes` k-steps from W on (further ones read as 0), the tile's from w_row on.
-  __device__ __forceinline__ Part part_cols(const bf16_t *X, int64_t ldx, int rows, const bf16_t *W, int n, int planes, int w_row) {
+  __device__ __forceinline__ Part part_at(const bf16_t *X, int64_t ldx, int rows, const bf16_t *W, int n, int planes, int w_row) {
     Part p;
     w_plane = (uint32_t)(n >> 5) * 4096u;
     rw = __builtin_amdgcn_make_buffer_rsrc((void *)W, 0, (int)((uint32_t)planes * w_plane), 0x00020000);
@@ -151,7 +151,7 @@ struct Tile {
 #pragma unroll
     for (int i = i0; i < i1; ++i)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (lds_void *)(xs + st * STAGE + (wave * XI + i) * 512), 16, p.x_lane[i % XL],
-                                               KIND < TILE_COLS ? p.x_k + ks * (BK * 2) : ks * x_step + (wave * XI + i) * x_load, 0, 0);
+                                               KIND == TILE_ROWS ? p.x_k + ks * (BK * 2) : ks * x_step + (wave * XI + i) * x_load, 0, 0);
 #endif
   }
   __device__ __forceinline__ void load_w(const Part &p, int st, int ks, int b) {
@@ -218,8 +218,8 @@ struct Tile {
     __builtin_amdgcn_sched_barrier(0);
 #endif
   }
-  __device__ __forceinline__ float result(int a, int b, int i) const {
-    float v = 0.f;
+  __device__ __forceinline__ auto result(int a, int b, int i) const {
+    std::conditional_t<KIND == TILE_INT8, int32_t, float> v = 0;
 #ifdef __HIP_DEVICE_COMPILE__
     asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v) : "a"(acc[a][b][i]));
 #endif
@@ -400,5 +400,82 @@ struct Tile {
   }
 };
 
+// A tile of a product: operands as Tile::part_at has them, its k-steps (a multiple of four), and where its results go.
+struct Item {
+  const bf16_t *x, *w;
+  int64_t ldx;
+  int x_rows, w_n, w_planes, w_row, ksteps;
+  int kind, row0, col0;   // of the kernel's own
+};
+
+template <typename T>
+__device__ __forceinline__ typename T::Part part_of(T &t, const Item &i) { return t.part_at(i.x, i.ldx, i.x_rows, i.w, i.w_n, i.w_planes, i.w_row); }
+
+// One tile with the whole workgroup.
+template <typename T>
+__device__ __forceinline__ void one_tile(T &t, const Item &c) {
+  const auto p = part_of(t, c);
+  t.zero();
+  t.begin(p);
+  int ks = 0;
+  for (; ks < c.ksteps - 4; ks += 4) t.four(p, ks);
+  t.last_four(p, ks);
+}
+
+// Tiles one after the other, the next one's first k-steps under the last products of the one at hand.  take(item): the next tile, or false; a tile is
+// known one tile ahead, and ask() is called as a tile begins, in time for the take() behind it.  One loop of four k-steps for all of a tile: with last k-steps
+// of their own, behind the loop, the accumulators move between the two, and what spills meanwhile waits for every load in flight.
+template <typename T, typename Ask, typename Take, typename Done>
+__device__ __forceinline__ void walk(T &t, Ask ask, Take take, Done done) {
+  Item c, d;
+  if (!take(c)) return;
+  d = c;   // behind the last tile: its own first k-steps again, which nothing reads
+  bool more = take(d);
+  auto p = part_of(t, c);
+  t.zero();
+  t.begin(p);
+  ask();
+  for (;;) {
+    for (int ks = 0; ks >= 0;) {
+      t.template kstep<0, true, 3>(p, ks + 3);
+      ks += 4;
+      int at = ks;
+      if (ks >= c.ksteps) {
+        p = part_of(t, d);
+        at = 0;
+        ks = -1;
+      }
+      t.template kstep<1, true, 3>(p, at);
+      t.template kstep<2, true, 3>(p, at + 1);
+      t.template kstep<3, true, 3>(p, at + 2);
+    }
+    // what `done` computes from the lane alone is not to be held in registers through the k-steps
+    asm volatile("" : "+v"(t.lrow), "+v"(t.half));
+    t.settle();
+    done(c);
+    if (!more) break;
+    t.zero();
+    c = d;
+    more = take(d);
+    ask();
+  }
+  t.drain();
+}
+
+// two registers of four consecutive results each (bf16) against those of the other half of the wavefront: eight consecutive ones
+__device__ __forceinline__ uint4 eight(const uint32_t (&a)[2], const uint32_t (&b)[2]) {
+#ifdef __HIP_DEVICE_COMPILE__
+  typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+  const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(a[0], b[0], false, false));
+  const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(a[1], b[1], false, false));
+  return make_uint4(lo[0], hi[0], lo[1], hi[1]);
+#else
+  return uint4{};
+#endif
+}
+__device__ __forceinline__ uint32_t two_bf16(float a, float b) {
+  typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+  return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
+}
 }  // namespace
 }  // namespace pl

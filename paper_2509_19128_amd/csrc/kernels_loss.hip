@@ -83,55 +83,6 @@ __global__ __launch_bounds__(256) void loss_gather_kernel(Head q, int first, bf1
   }
 }
 
-// A tile of a product: operands as Tile::part_cols has them, its k-steps (a multiple of four), and where its results go.
-struct Item {
-  const bf16_t *x, *w;
-  int64_t ldx;
-  int x_rows, w_n, w_planes, w_row, ksteps;
-  int kind, row0, col0;   // of the kernel's own
-};
-
-// Tiles one after the other, the next one's first k-steps under the last products of the one at hand.  take(item): the next tile, or false; a tile is
-// known one tile ahead, and ask() is called as a tile begins, in time for the take() behind it.  One loop of four k-steps for all of a tile: with last k-steps
-// of their own, behind the loop, the accumulators move between the two, and what spills meanwhile waits for every load in flight.
-template <typename T, typename Ask, typename Take, typename Done>
-__device__ __forceinline__ void walk(T &t, Ask ask, Take take, Done done) {
-  auto part = [&](const Item &i) { return t.part_cols(i.x, i.ldx, i.x_rows, i.w, i.w_n, i.w_planes, i.w_row); };
-  Item c, d;
-  if (!take(c)) return;
-  d = c;   // behind the last tile: its own first k-steps again, which nothing reads
-  bool more = take(d);
-  auto p = part(c);
-  t.zero();
-  t.begin(p);
-  ask();
-  for (;;) {
-    for (int ks = 0; ks >= 0;) {
-      t.template kstep<0, true, 3>(p, ks + 3);
-      ks += 4;
-      int at = ks;
-      if (ks >= c.ksteps) {
-        p = part(d);
-        at = 0;
-        ks = -1;
-      }
-      t.template kstep<1, true, 3>(p, at);
-      t.template kstep<2, true, 3>(p, at + 1);
-      t.template kstep<3, true, 3>(p, at + 2);
-    }
-    // what `done` computes from the lane alone is not to be held in registers through the k-steps
-    asm volatile("" : "+v"(t.lrow), "+v"(t.half));
-    t.settle();
-    done(c);
-    if (!more) break;
-    t.zero();
-    c = d;
-    more = take(d);
-    ask();
-  }
-  t.drain();
-}
-
 // Logit tiles: 256 vocabulary entries from v_begin on x BN rows.  XCD i takes the i-th eighth of them; bands of 2048 rows, in a band vocabulary tile by
 // vocabulary tile, so that an XCD's units share few operands at a time.
 template <int BN>
@@ -173,7 +124,7 @@ __global__ __launch_bounds__(256) void loss_forward_kernel(Head q, const bf16_t 
   tiles.init(count, q.vocab);
   if (tiles.at >= tiles.end) return;
   T t;
-  t.init_cols(xs);
+  t.init_at(xs);
   walk(t, [] {}, [&](Item &d) {
     if (tiles.at >= tiles.end) return false;
     int mt, vt;
@@ -264,21 +215,6 @@ __global__ __launch_bounds__(1024) void loss_merge_kernel(const float2 *__restri
   logprob[t] = zt[r] - l;
 }
 
-// two registers of four consecutive results each (bf16) against those of the other half of the wavefront: eight consecutive ones
-__device__ __forceinline__ uint4 eight(const uint32_t (&a)[2], const uint32_t (&b)[2]) {
-#ifdef __HIP_DEVICE_COMPILE__
-  typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
-  const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(a[0], b[0], false, false));
-  const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(a[1], b[1], false, false));
-  return make_uint4(lo[0], hi[0], lo[1], hi[1]);
-#else
-  return uint4{};
-#endif
-}
-__device__ __forceinline__ uint32_t two_bf16(float a, float b) {
-  typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
-  return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
-}
 // a 32 x 32 block of results (a lane: one column, rows (i / 4) * 8 + half * 4 + i % 4) as two fragments of eight consecutive rows: 16 f + 8 half on
 __device__ __forceinline__ void fragments(uint4 (&f)[2], const float (&v)[16]) {
 #pragma unroll
@@ -310,7 +246,7 @@ __global__ __launch_bounds__(256) void loss_grad_logits_kernel(Head q, const bf1
   tiles.init(*q.count, n_v);
   if (tiles.at >= tiles.end) return;
   T t;
-  t.init_cols(xs);
+  t.init_at(xs);
   walk(t, [] {}, [&](Item &d) {
     if (tiles.at >= tiles.end) return false;
     int mt, vt;
@@ -430,7 +366,7 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(Head q, GradParams g) {
   __syncthreads();
   if (drawn[0] < 0) return;
   T t;
-  t.init_cols(xs);
+  t.init_at(xs);
   int turn = 0;
   walk(t, [&] {
     if (threadIdx.x == 0) drawn[turn] = draw();   // for the tile behind the next: its place was read a tile ago, and is read again behind this tile's barriers
