@@ -27,45 +27,63 @@ __device__ inline int quotient(float x, float s, float inv) {
   return (int)fminf(fmaxf(q, -127.f), 127.f);
 }
 // What the codes of a row need, from its largest magnitude (infinity: a number that is none): the scale, and the factors of quotient().  Tiny rows: both
-// sides of the quotient times a power of two, so that 1 / s is finite.
+// sides of the quotient times a power of two, so that 1 / s is finite; they, zeros and rows that hold no numbers take the long way.
 struct RowScale {
   float scale, s, inv, up;
+  bool plain;
   __device__ inline explicit RowScale(float most) {
     const bool fine = most < INFINITY;
     scale = fine ? most / 127.f : NAN;
-    up = scale < 0x1p-100f ? 0x1p100f : 1.f;
+    plain = scale >= 0x1p-100f;
+    up = plain ? 1.f : 0x1p100f;
     s = fine ? scale * up : 0.f;
     inv = s > 0.f ? 1.f / s : 0.f;
   }
-  __device__ inline int code(float x) const { return inv > 0.f ? quotient(x * up, s, inv) : 0; }
+  // The codes of four values, a byte each.  x / s + 1.5 2^23 in one rounding has the code in its last byte; where a remainder is half of s or more
+  // the quotient was rounded next to a tie, and the careful one decides.
+  __device__ __forceinline__ uint32_t four(float x0, float x1, float x2, float x3) const {
+    constexpr float MAGIC = 12582912.f;
+    const float t0 = fmaf(x0, inv, MAGIC), t1 = fmaf(x1, inv, MAGIC), t2 = fmaf(x2, inv, MAGIC), t3 = fmaf(x3, inv, MAGIC);
+    const float r0 = fmaf(MAGIC - t0, s, x0), r1 = fmaf(MAGIC - t1, s, x1), r2 = fmaf(MAGIC - t2, s, x2), r3 = fmaf(MAGIC - t3, s, x3);
+    const float r = fmaxf(fmaxf(fabsf(r0), fabsf(r1)), fmaxf(fabsf(r2), fabsf(r3)));
+    if (plain && r < 0.5f * s) {
+      const uint32_t lo = __builtin_amdgcn_perm(__float_as_uint(t1), __float_as_uint(t0), 0x0c0c0400u), hi = __builtin_amdgcn_perm(__float_as_uint(t3), __float_as_uint(t2), 0x0c0c0400u);
+      return hi << 16 | lo;
+    }
+    if (!(inv > 0.f)) return 0;
+    return ((uint32_t)quotient(x0 * up, s, inv) & 255u) | ((uint32_t)quotient(x1 * up, s, inv) & 255u) << 8 | ((uint32_t)quotient(x2 * up, s, inv) & 255u) << 16 |
+           (uint32_t)quotient(x3 * up, s, inv) << 24;
+  }
 };
 __device__ inline float magnitude(float x, float m) {   // infinity stands for NaN too
   const float a = fabsf(x);
   return a < INFINITY ? fmaxf(m, a) : INFINITY;
 }
-// sixteen values of a row
-template <typename T>
-struct Sixteen {
-  uint4 raw[sizeof(T)];
+// COUNT consecutive values of a row
+template <typename T, int COUNT>
+struct Values {
+  static constexpr int VECTORS = COUNT * sizeof(T) / 16;
+  uint4 raw[VECTORS];
   __device__ __forceinline__ void load(const T *p) {
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(T); ++i) raw[i] = ((const uint4 *)p)[i];
+    for (int i = 0; i < VECTORS; ++i) raw[i] = ((const uint4 *)p)[i];
   }
-  __device__ __forceinline__ float get(int i) const { return (float)((const T *)raw)[i]; }
+  __device__ __forceinline__ float get(int i) const {
+    constexpr int PER = 16 / sizeof(T);
+    const uint4 u = raw[i / PER];
+    const int w = i % PER * sizeof(T) / 4;
+    const uint32_t d = w == 0 ? u.x : w == 1 ? u.y : w == 2 ? u.z : u.w;
+    if constexpr (sizeof(T) == 4) return __uint_as_float(d);
+    else return __uint_as_float(i & 1 ? d & 0xffff0000u : d << 16);
+  }
   __device__ __forceinline__ float most(float m) const {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) m = magnitude(get(i), m);
+    for (int i = 0; i < COUNT; ++i) m = magnitude(get(i), m);
     return m;
   }
-  __device__ __forceinline__ uint4 codes(const RowScale &r) const {
-    uint32_t q[4];
+  __device__ __forceinline__ void codes(const RowScale &r, uint32_t (&q)[COUNT / 4]) const {
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      q[w] = 0;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) q[w] |= ((uint32_t)r.code(get(w * 4 + e)) & 255u) << (8 * e);
-    }
-    return make_uint4(q[0], q[1], q[2], q[3]);
+    for (int w = 0; w < COUNT / 4; ++w) q[w] = r.four(get(w * 4), get(w * 4 + 1), get(w * 4 + 2), get(w * 4 + 3));
   }
 };
 
@@ -75,7 +93,7 @@ template <typename T, int HELD>
 __global__ __launch_bounds__(1024) void quantize_weights_kernel(const T *__restrict__ w, int64_t ldw, uint4 *__restrict__ q, float *__restrict__ scale, int N, int K) {
   const int r = threadIdx.x & 7, row = blockIdx.x * 8 + r, lanes = blockDim.x >> 3, first = threadIdx.x >> 3, pieces = K >> 4;
   w += row * ldw;
-  Sixteen<T> held[HELD ? HELD : 1];
+  Values<T, 16> held[HELD ? HELD : 1];
   float m = 0.f;
   if constexpr (HELD > 0) {
 #pragma unroll
@@ -99,8 +117,10 @@ __global__ __launch_bounds__(1024) void quantize_weights_kernel(const T *__restr
   for (int i = 0; i < (int)blockDim.x >> 6; ++i) m = fmaxf(m, part[i][r]);
   const RowScale rs(m);
   if (first == 0) scale[row] = rs.scale;
-  auto store = [&](int p, const Sixteen<T> &v) {   // piece p is (k / 16): block p / 8, half (p / 4) % 2, quarter p % 4
-    q[(((int64_t)(p >> 3) * (N >> 5) + (row >> 5)) * 4 + (p & 3)) * 64 + ((p >> 2) & 1) * 32 + (row & 31)] = v.codes(rs);
+  auto store = [&](int p, const Values<T, 16> &v) {   // piece p is (k / 16): block p / 8, half (p / 4) % 2, quarter p % 4
+    uint32_t c[4];
+    v.codes(rs, c);
+    q[(((int64_t)(p >> 3) * (N >> 5) + (row >> 5)) * 4 + (p & 3)) * 64 + ((p >> 2) & 1) * 32 + (row & 31)] = make_uint4(c[0], c[1], c[2], c[3]);
   };
   if constexpr (HELD > 0) {
 #pragma unroll
@@ -114,15 +134,15 @@ __global__ __launch_bounds__(1024) void quantize_weights_kernel(const T *__restr
   }
 }
 
-// Codes of x, row-major, rows padded with zeros to k_pad.  A workgroup per row.
-__global__ __launch_bounds__(1024) void quantize_rows_kernel(const bf16_t *__restrict__ x, int64_t ldx, uint4 *__restrict__ q, float *__restrict__ scale, int K, int k_pad) {
+// Codes of x, row-major, rows padded with zeros to k_pad.  A workgroup per row, eight values of a lane at a time.
+__global__ __launch_bounds__(1024) void quantize_rows_kernel(const bf16_t *__restrict__ x, int64_t ldx, uint2 *__restrict__ q, float *__restrict__ scale, int K, int k_pad) {
   x += blockIdx.x * ldx;
-  q += (int64_t)blockIdx.x * (k_pad >> 4);
-  const int pieces = K >> 4;
-  Sixteen<bf16_t> v;
+  q += (int64_t)blockIdx.x * (k_pad >> 3);
+  const int pieces = K >> 3;
+  Values<bf16_t, 8> v;
   float m = 0.f;
   for (int p = threadIdx.x; p < pieces; p += blockDim.x) {
-    v.load(x + p * 16);
+    v.load(x + p * 8);
     m = v.most(m);
   }
   __shared__ float part[16];
@@ -132,9 +152,11 @@ __global__ __launch_bounds__(1024) void quantize_rows_kernel(const bf16_t *__res
   for (int i = 0; i < (int)blockDim.x >> 6; ++i) m = fmaxf(m, part[i]);
   const RowScale rs(m);
   if (threadIdx.x == 0) scale[blockIdx.x] = rs.scale;
-  for (int p = threadIdx.x; p < k_pad >> 4; p += blockDim.x) {
-    if (p < pieces && pieces > (int)blockDim.x) v.load(x + p * 16);   // (otherwise the one piece is still here)
-    q[p] = p < pieces ? v.codes(rs) : make_uint4(0, 0, 0, 0);
+  for (int p = threadIdx.x; p < k_pad >> 3; p += blockDim.x) {
+    if (p < pieces && pieces > (int)blockDim.x) v.load(x + p * 8);   // (otherwise the one piece is still here)
+    uint32_t c[2] = {0, 0};
+    if (p < pieces) v.codes(rs, c);
+    q[p] = make_uint2(c[0], c[1]);
   }
 }
 
@@ -218,9 +240,9 @@ __device__ __forceinline__ void int8_store(const T &t, const Int8Params &g, cons
 }
 
 // A tile per workgroup; the row tiles of a column tile and slice sit 8 ids apart, so that they run on one XCD at the same time and share W's way there.
-template <int WM, int WN, int AT, int BT, int OUT>
+template <int WM, int WN, int AT, int BT, int OUT, bool COLD>
 __global__ __launch_bounds__(256) void gemm_int8_kernel(Int8Params g) {
-  typedef Tile<WM, WN, AT, BT, false, TILE_INT8> T;
+  typedef Tile<WM, WN, AT, BT, COLD, TILE_INT8> T;
   __shared__ __attribute__((aligned(1024))) bf16_t xs[T::LDS];
   const int item = (blockIdx.x / (8 * g.nrow)) * 8 + (blockIdx.x & 7), rtile = (blockIdx.x >> 3) % g.nrow;
   if (item >= g.ncol * g.splits) return;
@@ -270,37 +292,146 @@ __global__ __launch_bounds__(256) void int8_slices_kernel(const i32x4 *__restric
   else *(uint2 *)(y + (int64_t)m * N + n) = make_uint2(two_bf16(r[0], r[1]), two_bf16(r[2], r[3]));
 }
 
+// Few rows (at most ROWS) in one launch: a workgroup quantises them for itself into LDS, under its first loads of W, and owns 32 channels. Eight wavefronts take
+// turns of 1 KiB of W (32 channels x 2 x 16 k in operand order: a lane has sixteen codes of one channel), against which each row's codes come
+// from LDS, the same for half a wavefront.  Bound by W's way from memory.
+template <int ROWS, typename T>
+__global__ __launch_bounds__(512) void gemm_int8_few_kernel(const bf16_t *__restrict__ x, int64_t ldx, const int8_t *__restrict__ wq, const float *__restrict__ sw, T *__restrict__ y,
+                                                            int M, int N, int K) {
+  constexpr int AHEAD = 8;   // turns of a wavefront whose loads are in flight
+  extern __shared__ __attribute__((aligned(16))) int8_t codes[];   // [ROWS][K]
+  __shared__ float part[8], scale[ROWS];
+  __shared__ int32_t sums[8][ROWS][32];
+  const int l = threadIdx.x & 63, wave = threadIdx.x >> 6, turns = K >> 8;
+  const i32x4 *w = (const i32x4 *)(wq + ((int64_t)(wave >> 2) * (N >> 5) + blockIdx.x) * 4096 + (wave & 3) * 1024) + l;
+  const int64_t step = (int64_t)N * 16;   // 256 k on, in vectors
+  i32x4 cur[AHEAD], nxt[AHEAD];
+#pragma unroll
+  for (int u = 0; u < AHEAD; ++u)
+    if (u < turns) cur[u] = __builtin_nontemporal_load(w + u * step);
+
+  // wavefronts share the rows: 512 / ROWS lanes each
+  constexpr int WAVES = 8 / ROWS;
+  const int pieces = K >> 3, row = wave / WAVES, first = threadIdx.x & (64 * WAVES - 1);
+  x += min(row, M - 1) * ldx;
+  Values<bf16_t, 8> v;
+  float m = 0.f;
+  for (int p = first; p < pieces; p += 64 * WAVES) {
+    v.load(x + p * 8);
+    m = v.most(m);
+  }
+  m = wave_max(m);
+  if (l == 0) part[wave] = m;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < WAVES; ++i) m = fmaxf(m, part[row * WAVES + i]);
+  const RowScale rs(m);
+  if (first == 0) scale[row] = rs.scale;
+  for (int p = first; p < pieces; p += 64 * WAVES) {
+    if (pieces > 64 * WAVES) v.load(x + p * 8);
+    uint32_t c[2];
+    v.codes(rs, c);
+    *(uint2 *)(codes + row * K + p * 8) = make_uint2(c[0], c[1]);
+  }
+  __syncthreads();
+
+  int32_t sum[ROWS];
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) sum[r] = 0;
+  const int8_t *mine = codes + (wave >> 2) * 128 + (l >> 5) * 64 + (wave & 3) * 16;
+  for (int t0 = 0; t0 < turns; t0 += AHEAD) {
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+      if (t0 + AHEAD + u < turns) nxt[u] = __builtin_nontemporal_load(w + (t0 + AHEAD + u) * step);
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+      if (t0 + u < turns) {
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+          const i32x4 c = *(const i32x4 *)(mine + r * K + (t0 + u) * 256);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sum[r] = __builtin_amdgcn_sdot4(cur[u][e], c[e], sum[r], false);
+        }
+      }
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) cur[u] = nxt[u];
+  }
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    sum[r] = with_xor32(sum[r], [](int a, int b) { return a + b; });
+    if (l < 32) sums[wave][r][l] = sum[r];
+  }
+  __syncthreads();
+  const int r = threadIdx.x >> 5, n = blockIdx.x * 32 + (threadIdx.x & 31);
+  if (r >= ROWS || r >= M) return;
+  int32_t s = 0;
+  for (int i = 0; i < 8; ++i) s += sums[i][r][threadIdx.x & 31];
+  y[(int64_t)r * N + n] = (T)((float)s * scale[r] * sw[n]);
+}
+
 int done() { return hipGetLastError() == hipSuccess ? 0 : -7; }
 int64_t align256(int64_t b) { return (b + 255) / 256 * 256; }
 
-// How a product is cut: tile shape and K slices.
-enum { I8_32x128, I8_64x128, I8_128x128, I8_128x256, I8_256x128, I8_64x64, I8_ROUNDS };
+// How a product is cut: tile shape and K slices.  Microseconds as measured: fixed + k-steps of a slice * (base + load * (fraction of the units at work) +
+// more * (average beyond one workgroup per unit) + round * (workgroups of the fullest unit - 1)), out per MB of bf16 results, and with slices their
+// launch and MB of sums.  Fitted to 2700 launches (the products of the 1.5B, 7B and 32B shapes and smaller ones, 1 to 3001 rows, 1 to 24 slices, weights
+// not in the last-level cache): the choice takes 1.2 % more than the best measured one on average, 6 % in 95 of 100.
+enum { I8_32x128, I8_64x128, I8_128x128, I8_128x256, I8_64x64, I8_ROUNDS };
+struct ShapeTime { int rows, cols; float fixed, base, load, more, round, slices, slice_mb, out_mb; };
+constexpr ShapeTime SHAPES[] = {{32, 128, 5.29f, 0.275f, 0.137f, 0.128f, 0.217f, 4.46f, 0.203f, 0.f},   {64, 128, 5.88f, 0.324f, 0.197f, 0.155f, 0.25f, 3.67f, 0.371f, 0.f},
+                                {128, 128, 7.75f, 0.359f, 0.289f, 0.278f, 0.313f, 2.88f, 0.386f, 0.098f}, {128, 256, 8.39f, 0.625f, 0.623f, 0.419f, 0.707f, 2.75f, 0.337f, 0.067f},
+                                {64, 64, 5.53f, 0.21f, 0.117f, 0.123f, 0.17f, 2.6f, 0.434f, 0.f},          {256, 256, 21.f, 0.98f, 0.393f, 0.407f, 1.258f, 0.f, 0.f, 0.377f}};
 struct Int8Plan { int shape, splits, slice; };
-constexpr int SHAPE_ROWS[] = {32, 64, 128, 128, 256, 64, 256}, SHAPE_COLS[] = {128, 128, 128, 256, 128, 64, 256};
 Int8Plan int8_plan(int M, int N, int K) {
   const int groups = (K + K_UNIT - 1) / K_UNIT;
-  int shape = M <= 32 ? I8_32x128 : M <= 64 ? I8_64x128 : M <= 128 ? I8_128x128 : M <= 256 ? I8_256x128 : I8_ROUNDS;
-  int splits = 1;
-  if (shape != I8_ROUNDS) {
-    const int tiles = (M + SHAPE_ROWS[shape] - 1) / SHAPE_ROWS[shape] * ((N + SHAPE_COLS[shape] - 1) / SHAPE_COLS[shape]);
-    splits = std::max(1, std::min(groups, UNITS / tiles));
+  const float mb = 1e-6f * M * N;
+  Int8Plan best{-1, 1, 0};
+  float best_us = 0;
+  for (int shape = 0; shape <= I8_ROUNDS; ++shape) {
+    const ShapeTime &f = SHAPES[shape];
+    // tiles of mostly absent rows, and so many small ones that their W is read over and over, were not measured
+    if ((f.rows > 64 && f.rows >= 4 * M) || (shape != I8_ROUNDS && (int64_t)f.rows * 24 < M)) continue;
+    const int64_t tiles = (int64_t)((M + f.rows - 1) / f.rows) * ((N + f.cols - 1) / f.cols);
+    for (int sp : {1, 2, 3, 4, 5, 6, 8, 9, 12, 16, 24}) {
+      if (sp > groups || (sp > 1 && (shape == I8_ROUNDS || tiles * sp > 600))) break;
+      const int per = (groups + sp - 1) / sp, splits = (groups + per - 1) / per;   // (no empty slice)
+      const int64_t n = tiles * splits;
+      const float r = n * (1.f / UNITS);
+      float us = f.fixed + per * 4 * (f.base + f.load * std::min(r, 1.f) + f.more * std::max(r - 1, 0.f) + f.round * ((n + UNITS - 1) / UNITS - 1)) + f.out_mb * 2 * mb;
+      if (splits > 1) us += f.slices + f.slice_mb * 4 * splits * mb;
+      if (best.shape < 0 || us < best_us) {
+        best = Int8Plan{shape, splits, per * 4};
+        best_us = us;
+      }
+    }
   }
-  const int per = (groups + splits - 1) / splits;
-  return Int8Plan{shape, (groups + per - 1) / per, per * 4};   // (no empty slice)
+  return best;
+}
+
+// Calls of gemm_int8_few_kernel.  What every workgroup does for itself grows with rows x K and with the number of workgroups: us, in one launch / in
+// two, 1 row 4608 x 3584 6.6 / 10.7, 37888 x 3584 26.9 / 29.6, 55296 x 5120 46.4 / 44.9, 3584 x 18944 20.2 / 19.1; 2 rows 4608 x 3584 7.7 / 11.0, 1536 x
+// 8960 14.7 / 11.2; 4 rows 4608 x 3584 8.8 / 10.5, 17920 x 1536 11.1 / 10.0; tiny shape 4.5 / 7.0.
+bool int8_few(int M, int N, int K) {
+  const int rows = M > 2 ? 4 : M;
+  return M <= 4 && rows * K <= 16384 && rows * N <= 45000;
 }
 
 template <int WM, int WN, int AT, int BT>
-void launch_shape(const Int8Params &g, int out, hipStream_t s) {
-  const dim3 grid((g.ncol * g.splits + 7) / 8 * 8 * g.nrow);
-  if (out == OUT_F32) hipLaunchKernelGGL((gemm_int8_kernel<WM, WN, AT, BT, OUT_F32>), grid, dim3(256), 0, s, g);
-  else if (out == OUT_BF16) hipLaunchKernelGGL((gemm_int8_kernel<WM, WN, AT, BT, OUT_BF16>), grid, dim3(256), 0, s, g);
-  else hipLaunchKernelGGL((gemm_int8_kernel<WM, WN, AT, BT, OUT_SLICES>), grid, dim3(256), 0, s, g);
+void launch_shape(const Int8Params &g, int out, bool cold, hipStream_t s) {
+  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((g.ncol * g.splits + 7) / 8 * 8 * g.nrow), dim3(256), 0, s, g); };
+  auto with = [&](auto COLD) {
+    constexpr bool c = WM == 1 && decltype(COLD)::value;
+    if (out == OUT_F32) launch(gemm_int8_kernel<WM, WN, AT, BT, OUT_F32, c>);
+    else if (out == OUT_BF16) launch(gemm_int8_kernel<WM, WN, AT, BT, OUT_BF16, c>);
+    else launch(gemm_int8_kernel<WM, WN, AT, BT, OUT_SLICES, c>);
+  };
+  if (cold) with(std::true_type{}); else with(std::false_type{});
 }
 
 template <typename T>
 void launch_weights(const T *w, int64_t ldw, int8_t *q, float *scale, int N, int K, hipStream_t s) {
-  // lanes of a row so that it takes at most HELD pieces of a lane: 32, 64 or 128
-  constexpr int HELD = sizeof(T) == 4 ? 4 : 8;
+  // lanes of a row so that it takes at most HELD pieces of a lane: 32, 64 or 128 (more pieces would not fit a lane's 128 registers)
+  constexpr int HELD = sizeof(T) == 4 ? 5 : 7;
   const int pieces = K / 16, lanes = pieces <= 32 * HELD ? 32 : pieces <= 64 * HELD ? 64 : 128;
   auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(N / 8), dim3(lanes * 8), 0, s, w, ldw, (uint4 *)q, scale, N, K); };
   if (pieces <= lanes * HELD) launch(quantize_weights_kernel<T, HELD>);
@@ -321,22 +452,36 @@ int64_t gemm_int8_workspace_bytes(int M, int N, int K) {
 }
 
 int launch_gemm_int8(const bf16_t *x, int64_t ldx, const int8_t *wq, const float *sw, void *y, bool f32, int M, int N, int K, void *ws, hipStream_t s) {
+  if (int8_few(M, N, K)) {
+    auto launch = [&](auto kernel, auto *out) { hipLaunchKernelGGL(kernel, dim3(N / 32), dim3(512), (M > 2 ? 4 : M) * K, s, x, ldx, wq, sw, out, M, N, K); };
+    auto with = [&](auto *out) {
+      typedef std::remove_pointer_t<decltype(out)> T;
+      if (M == 1) launch(gemm_int8_few_kernel<1, T>, out);
+      else if (M == 2) launch(gemm_int8_few_kernel<2, T>, out);
+      else launch(gemm_int8_few_kernel<4, T>, out);
+    };
+    if (f32) with((float *)y); else with((bf16_t *)y);
+    return done();
+  }
   const Int8Plan plan = int8_plan(M, N, K);
   const int k_pad = (K + K_UNIT - 1) / K_UNIT * K_UNIT;
   float *sx = (float *)ws;
   int8_t *xq = (int8_t *)ws + align256((int64_t)M * 4);
   int32_t *slices = (int32_t *)(xq + align256((int64_t)M * k_pad));
-  hipLaunchKernelGGL(quantize_rows_kernel, dim3(M), dim3(std::min(1024, (K / 16 + 63) / 64 * 64)), 0, s, x, ldx, (uint4 *)xq, sx, K, k_pad);
+  hipLaunchKernelGGL(quantize_rows_kernel, dim3(M), dim3(std::min(1024, (K / 8 + 63) / 64 * 64)), 0, s, x, ldx, (uint2 *)xq, sx, K, k_pad);
   Int8Params g{xq, wq, sx, sw, plan.splits > 1 ? (void *)slices : y, M, N, K, k_pad, plan.splits, plan.slice,
-               (N + SHAPE_COLS[plan.shape] - 1) / SHAPE_COLS[plan.shape], (M + SHAPE_ROWS[plan.shape] - 1) / SHAPE_ROWS[plan.shape]};
+               (N + SHAPES[plan.shape].cols - 1) / SHAPES[plan.shape].cols, (M + SHAPES[plan.shape].rows - 1) / SHAPES[plan.shape].rows};
   const int out = plan.splits > 1 ? OUT_SLICES : f32 ? OUT_F32 : OUT_BF16;
+  // Weights read once in the call, of a matrix so large that a model of such does not stay in the last-level cache between two steps, by non-temporal
+  // loads: 1 row 55296 x 5120 52.8 -> 47.2 us, 37888 x 3584 33.9 -> 31.4, 128 rows 55296 x 5120 61.5 -> 57.2 (one matrix again and again out of the
+  // cache: up to 10 % the other way, 37888 x 3584, 64 rows, 30 -> 33).
+  const bool cold = g.nrow == 1 && (int64_t)N * K > (8 << 20);
   switch (plan.shape) {
-    case I8_32x128: launch_shape<1, 4, 1, 1>(g, out, s); break;
-    case I8_64x128: launch_shape<1, 4, 2, 1>(g, out, s); break;
-    case I8_128x128: launch_shape<1, 4, 4, 1>(g, out, s); break;
-    case I8_128x256: launch_shape<1, 4, 4, 2>(g, out, s); break;
-    case I8_256x128: launch_shape<1, 4, 8, 1>(g, out, s); break;
-    case I8_64x64: launch_shape<2, 2, 1, 1>(g, out, s); break;
+    case I8_32x128: launch_shape<1, 4, 1, 1>(g, out, cold, s); break;
+    case I8_64x128: launch_shape<1, 4, 2, 1>(g, out, cold, s); break;
+    case I8_128x128: launch_shape<1, 4, 4, 1>(g, out, cold, s); break;
+    case I8_128x256: launch_shape<1, 4, 4, 2>(g, out, cold, s); break;
+    case I8_64x64: launch_shape<2, 2, 1, 1>(g, out, cold, s); break;
     default:
       if (out == OUT_F32) hipLaunchKernelGGL(gemm_int8_rounds_kernel<OUT_F32>, dim3(UNITS), dim3(256), 0, s, g);
       else hipLaunchKernelGGL(gemm_int8_rounds_kernel<OUT_BF16>, dim3(UNITS), dim3(256), 0, s, g);
