@@ -52,6 +52,7 @@ struct Tile {
   static constexpr int BM = WM * AT * 32, BN = WN * BT * 32;
   static constexpr int XI = BM / 32, XH = (XI + 1) / 2, WI = BT * 4;   // loads of a wavefront per k-step: x (half of them XH), W
   static constexpr int STAGE = BM * BK, LDS = STAGES * STAGE;          // elements
+  static constexpr int X_CACHE = KIND == TILE_COLS && COLD ? 2 : 0;   // (weights are x there; non-temporal where nothing reads them again)
   // Offsets of x held per lane: one per load; of the kinds that address whole tiles, those that differ by more than a number of rows, which a scalar
   // adds (their kernels have no register to spare: a spill in the main loop waits for every load in flight).
   static constexpr int XL = KIND == TILE_ROWS ? XI : KIND != TILE_COLS_T ? 1 : BM == 256 ? 2 : 1;
@@ -151,7 +152,7 @@ struct Tile {
 #pragma unroll
     for (int i = i0; i < i1; ++i)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (lds_void *)(xs + st * STAGE + (wave * XI + i) * 512), 16, p.x_lane[i % XL],
-                                               KIND == TILE_ROWS ? p.x_k + ks * (BK * 2) : ks * x_step + (wave * XI + i) * x_load, 0, 0);
+                                               KIND == TILE_ROWS ? p.x_k + ks * (BK * 2) : ks * x_step + (wave * XI + i) * x_load, 0, X_CACHE);
 #endif
   }
   __device__ __forceinline__ void load_w(const Part &p, int st, int ks, int b) {

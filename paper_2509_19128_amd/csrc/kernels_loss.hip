@@ -28,31 +28,46 @@ constexpr float LOG2E = 1.4426950408889634f;
 
 struct Row { float inv_t, lse, scale; int32_t target; };   // scale = g inv_t; padding: all 0, target -1
 
-// positions with a target in order, their number, the way back, and zeros for the others
-__global__ __launch_bounds__(1024) void loss_rows_kernel(const int32_t *__restrict__ target, int32_t *__restrict__ count, int32_t *__restrict__ rows,
-                                                         int32_t *__restrict__ place, float *__restrict__ logprob, float *__restrict__ lse, int n, int vocab) {
-  __shared__ int32_t part[16];
+// The workgroup numbers the positions with a target in order: each(position, has, number) for every position; returns how many there are.
+template <int THREADS, typename Each>
+__device__ __forceinline__ int number_positions(const int32_t *__restrict__ target, int n, int vocab, Each each) {
+  __shared__ int32_t part[THREADS / 64];
   int base = 0;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int t0 = 0; t0 < n; t0 += 1024) {
+  for (int t0 = 0; t0 < n; t0 += THREADS) {
     const int t = t0 + threadIdx.x;
-    const bool in = t < n, has = in && (uint32_t)target[t] < (uint32_t)vocab;
+    const bool has = t < n && (uint32_t)target[t] < (uint32_t)vocab;
     const uint64_t mask = __ballot(has);
     if (lane == 0) part[wave] = __popcll(mask);
     __syncthreads();
     int at = base, all = 0;
-    for (int i = 0; i < 16; ++i) {
+#pragma unroll
+    for (int i = 0; i < THREADS / 64; ++i) {
       if (i < wave) at += part[i];
       all += part[i];
     }
-    at += __popcll(mask & (((uint64_t)1 << lane) - 1));
-    if (has) rows[at] = t;
-    if (in && place) place[t] = has ? at : -1;
-    if (in && logprob && !has) logprob[t] = lse[t] = 0.f;
+    if (t < n) each(t, has, at + __popcll(mask & (((uint64_t)1 << lane) - 1)));
     base += all;
     __syncthreads();
   }
-  if (threadIdx.x == 0) *count = base;
+  return base;
+}
+
+// What is known of the positions: how many have a target, which, and the way back (place, may be null); zeros for the others (logprob and lse may be null).
+struct Positions {
+  const int32_t *target;
+  int32_t *count, *rows, *place;
+  float *logprob, *lse;
+  int n, vocab;
+  __device__ __forceinline__ void note(int t, bool has, int number) const {
+    if (has) rows[number] = t;
+    if (place) place[t] = has ? number : -1;
+    if (logprob && !has) logprob[t] = lse[t] = 0.f;
+  }
+};
+__global__ __launch_bounds__(1024) void loss_rows_kernel(Positions q) {
+  const int count = number_positions<1024>(q.target, q.n, q.vocab, [&](int t, bool has, int number) { q.note(t, has, number); });
+  if (threadIdx.x == 0) *q.count = count;
 }
 
 struct Head {
@@ -65,10 +80,25 @@ struct Head {
 };
 
 // Rows [first, first + 32 * gridDim.x) in operand order (planes of 64 k, blocks of 32 rows; padding 0), as they are (copy, if any), and what
-// the tiles want to know of each.
-__global__ __launch_bounds__(256) void loss_gather_kernel(Head q, int first, bf16_t *__restrict__ op, bf16_t *__restrict__ copy, Row *__restrict__ info) {
-  const int r0 = blockIdx.x * 32, count = *q.count - first, j = threadIdx.x >> 6, half = (threadIdx.x >> 5) & 1, r = r0 + (threadIdx.x & 31);
-  const int k = blockIdx.y * 64 + half * 32 + j * 8, t = r < count ? q.rows[first + r] : -1;
+// the tiles want to know of each.  NUMBER: few positions, which every workgroup numbers for itself instead of a launch ahead.
+template <bool NUMBER>
+__global__ __launch_bounds__(256) void loss_gather_kernel(Head q, Positions at, int first, bf16_t *__restrict__ op, bf16_t *__restrict__ copy, Row *__restrict__ info) {
+  const int r0 = blockIdx.x * 32, j = threadIdx.x >> 6, half = (threadIdx.x >> 5) & 1, r = r0 + (threadIdx.x & 31), k = blockIdx.y * 64 + half * 32 + j * 8;
+  int t = -1;
+  if constexpr (NUMBER) {
+    __shared__ int32_t mine[32];
+    if (threadIdx.x < 32) mine[threadIdx.x] = -1;
+    __syncthreads();
+    const bool note = blockIdx.x == 0 && blockIdx.y == 0;
+    const int count = number_positions<256>(at.target, at.n, at.vocab, [&](int u, bool has, int number) {
+      if (has && (uint32_t)(number - r0) < 32u) mine[number - r0] = u;
+      if (note) at.note(u, has, number);
+    });
+    if (note && threadIdx.x == 0) *at.count = count;
+    t = mine[threadIdx.x & 31];   // (number_positions ends behind a barrier; n >= 1)
+  } else if (r < *q.count - first) {
+    t = q.rows[first + r];
+  }
   const uint4 v = t >= 0 ? *(const uint4 *)(q.h + t * q.ldh + k) : make_uint4(0, 0, 0, 0);
   *(uint4 *)(op + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 2048 + threadIdx.x * 8) = v;
   if (copy) *(uint4 *)(copy + (int64_t)r * q.d + k) = v;
@@ -113,10 +143,11 @@ __device__ __forceinline__ Item logit_item(const Head &q, const bf16_t *op, int 
 }
 
 // (max, sum of exponentials) of each row and group of vocabulary entries; the logit of the target from the tile that has it
-template <int WM, int WN, int AT, int BT>
+// COLD: one tile of rows, so that W is read once.  1.5B shape, 61 positions: @COLD@.
+template <int WM, int WN, int AT, int BT, bool COLD>
 __global__ __launch_bounds__(256) void loss_forward_kernel(Head q, const bf16_t *__restrict__ op, const Row *__restrict__ info, float2 *__restrict__ parts, float *__restrict__ zt,
                                                            int first, int n_pad) {
-  typedef Tile<WM, WN, AT, BT, false, TILE_COLS> T;
+  typedef Tile<WM, WN, AT, BT, COLD, TILE_COLS> T;
   __shared__ __attribute__((aligned(1024))) bf16_t xs[T::LDS];
   const int count = min(*q.count - first, n_pad);
   if (count <= 0) return;
@@ -182,13 +213,14 @@ __global__ __launch_bounds__(256) void loss_forward_kernel(Head q, const bf16_t 
   });
 }
 
-// The groups of 64 rows joined: sixteen wavefronts take every sixteenth group in order, then their sixteen results are joined in order.
+// The groups of sixteen rows joined, by 64 threads per row: each takes every 64th group in order, then their results are joined, eight at a time, in
+// order.
 __global__ __launch_bounds__(1024) void loss_merge_kernel(const float2 *__restrict__ parts, const float *__restrict__ zt, const int32_t *__restrict__ rows,
                                                           const int32_t *__restrict__ count, float *__restrict__ logprob, float *__restrict__ lse, int groups, int first,
                                                           int n_pad) {
-  __shared__ float2 joined[16][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = blockIdx.x * 64 + lane, n = min(*count - first, n_pad);
-  if ((int)blockIdx.x * 64 >= n) return;
+  __shared__ float2 joined[64][16];
+  const int r16 = threadIdx.x & 15, at = threadIdx.x >> 4, r = blockIdx.x * 16 + r16, n = min(*count - first, n_pad);
+  if ((int)blockIdx.x * 16 >= n) return;
   // (no entries: -inf, 0; NaN stays)
   auto join = [](float &m, float &s, float2 p) {
     const float top = p.x > m || p.x != p.x ? p.x : m;
@@ -196,19 +228,26 @@ __global__ __launch_bounds__(1024) void loss_merge_kernel(const float2 *__restri
     s = s * __expf(m - top) + p.y * __expf(p.x - top);
     m = top;
   };
+  const float2 none = make_float2(-INFINITY, 0.f);
   float m = -INFINITY, s = 0.f;
-  if (r < n)
-    for (int g = wave; g < groups; g += 16 * 8) {
-      float2 p[8];
+  for (int g = at; g < groups; g += 64 * 8) {
+    float2 p[8];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) p[u] = g + u * 16 < groups ? parts[(int64_t)(g + u * 16) * n_pad + r] : make_float2(-INFINITY, 0.f);
+    for (int u = 0; u < 8; ++u) p[u] = g + u * 64 < groups && r < n ? parts[(int64_t)(g + u * 64) * n_pad + r] : none;
 #pragma unroll
-      for (int u = 0; u < 8; ++u) join(m, s, p[u]);
-    }
-  joined[wave][lane] = make_float2(m, s);
+    for (int u = 0; u < 8; ++u) join(m, s, p[u]);
+  }
+  joined[at][r16] = make_float2(m, s);
   __syncthreads();
-  if (wave || r >= n) return;
-  for (int i = 1; i < 16; ++i) join(m, s, joined[i][lane]);
+  if (at < 8) {
+    m = -INFINITY; s = 0.f;
+    for (int i = 0; i < 8; ++i) join(m, s, joined[at * 8 + i][r16]);
+  }
+  __syncthreads();
+  if (at < 8) joined[at][r16] = make_float2(m, s);
+  __syncthreads();
+  if (at || r >= n) return;
+  for (int i = 1; i < 8; ++i) join(m, s, joined[i][r16]);
   const float l = m + logf(s);
   const int t = rows[first + r];
   lse[t] = l;
@@ -233,17 +272,43 @@ __device__ __forceinline__ int64_t fragment_place(int row, int k32, int n, int f
   return ((((int64_t)(k32 >> 1) * (n >> 5) + row) * 4 + 2 * f + half) * 64 + (k32 & 1) * 32 + lrow) * 16;
 }
 
+// How the gradient is cut, from the number of rows, which the device knows: vocabulary tiles of a piece, tiles of a slice of dh along a piece, and slices.
+// A piece's G, both ways, takes at most `most` elements each (or one vocabulary tile's); its tiles of 256 rows are whole rounds of the units where there
+// are that many.  Slices of dh: until there are as many tiles as units (each is a sum of its own that is read and written per piece).
+struct GradCut {
+  int nm, piece, slice, slices, slices_most;   // (slices_most: of any piece of this many rows)
+  __host__ __device__ GradCut(int count, int v_tiles, int d, int64_t ldw, int64_t most) {
+    nm = (count + 255) / 256;
+    const int64_t fit = most / 65536 / (nm > 0 ? nm : 1), far = ((int64_t)1 << 30) / ldw / 256;   // (W's rows of a piece lie behind one 32-bit offset)
+    int64_t p = fit < far ? fit : far;
+    if (p < 1) p = 1;
+    if (nm > 0 && nm * p >= UNITS) p = nm * p / UNITS * UNITS / nm;
+    piece = p < v_tiles ? (int)p : v_tiles;
+    const int tiles = nm * (d / 256);
+    int s = tiles > 0 ? UNITS / tiles : 1;
+    s = s < 1 ? 1 : s > 16 ? 16 : s;
+    slices_most = s;
+    slice = (piece + s - 1) / s;
+    slices = (piece + slice - 1) / slice;
+  }
+};
+
 // G of vocabulary entries [v_begin, v_begin + n_v), in operand order both ways: `by_row` for dh (a row's entries are its k) and `by_entry` for dW (an entry's
 // rows are its k).  The second is the first's transpose by the matrix cores: a product with the unit matrix moves what a lane holds of a position
 // to the lane of the entry, exactly.  Clears the tickets of the kernel behind.
 template <int WM, int WN, int AT, int BT>
 __global__ __launch_bounds__(256) void loss_grad_logits_kernel(Head q, const bf16_t *__restrict__ op, const Row *__restrict__ info, bf16_t *__restrict__ by_row, bf16_t *__restrict__ by_entry,
-                                                               int v_begin, int n_v, int width, int n_pad, int32_t *__restrict__ tickets) {
+                                                               int index, int64_t most, int n_pad, int32_t *__restrict__ tickets) {
   typedef Tile<WM, WN, AT, BT, false, TILE_COLS> T;
   __shared__ __attribute__((aligned(1024))) bf16_t xs[T::LDS];
   if (blockIdx.x == 0 && threadIdx.x < 8) tickets[threadIdx.x * 32] = 0;
+  const int count = *q.count;
+  const GradCut cut(count, (q.vocab + TILE_V - 1) / TILE_V, q.d, q.ldw, most);
+  const int64_t begin = (int64_t)index * cut.piece * TILE_V;
+  if (begin >= q.vocab) return;
+  const int v_begin = (int)begin, width = cut.piece * TILE_V, n_rows = cut.nm * 256;
   LogitTiles<T::BN> tiles;
-  tiles.init(*q.count, n_v);
+  tiles.init(count, min(width, q.vocab - v_begin));
   if (tiles.at >= tiles.end) return;
   T t;
   t.init_at(xs);
@@ -285,7 +350,7 @@ __global__ __launch_bounds__(256) void loss_grad_logits_kernel(Head q, const bf1
         fragments(f, G);
         if (by_row) {
 #pragma unroll
-          for (int k = 0; k < 2; ++k) *(uint4 *)((char *)by_row + fragment_place(m32, v32, n_pad, k, t.half, t.lrow)) = f[k];
+          for (int k = 0; k < 2; ++k) *(uint4 *)((char *)by_row + fragment_place(m32, v32, n_rows, k, t.half, t.lrow)) = f[k];
         }
         if (by_entry) {
           f32x16 turned;
@@ -312,10 +377,11 @@ __global__ __launch_bounds__(256) void loss_grad_logits_kernel(Head q, const bf1
 
 struct GradParams {
   const bf16_t *by_row, *by_entry, *copy;   // G both ways, h's rows
-  float *dh32;                              // [slices][n_pad][d], or null: no dh
+  float *dh32;                              // [slices][rows, to a multiple of 256][d], or null: no dh
   bf16_t *dw;                               // or null
   int32_t *tickets;                         // eight, 128 bytes apart, zero
-  int v_begin, n_v, width, n_pad, k_slice, tile_rows;   // k_slice: k-steps of a slice of dh; tile_rows: of the kernel that made G (rows beyond its last tile hold nothing)
+  int64_t most;
+  int index, n_pad, tile_rows;              // the piece; rows of `copy`; rows of a tile of the kernel that made G (beyond its last tile there is nothing)
 };
 
 // dh += G W and dW = G^T h of a piece of the vocabulary, 256 x 256 tiles of both in one launch: the units take them by tickets, those of dh, which
@@ -326,9 +392,13 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(Head q, GradParams g) {
   __shared__ __attribute__((aligned(1024))) bf16_t xs[T::LDS + 4];
   typedef __attribute__((address_space(3))) volatile int32_t lds_int;
   lds_int *drawn = (lds_int *)(xs + T::LDS);
-  const int count = *q.count, nd = q.d / 256, nm = (count + 255) / 256, nv = (g.n_v + TILE_V - 1) / TILE_V;
+  const int count = *q.count, nd = q.d / 256;
+  const GradCut cut(count, (q.vocab + TILE_V - 1) / TILE_V, q.d, q.ldw, g.most);
+  const int64_t begin = (int64_t)g.index * cut.piece * TILE_V;
+  if (begin >= q.vocab) return;
+  const int v_begin = (int)begin, nm = cut.nm, nv = min(cut.piece, (q.vocab - v_begin + TILE_V - 1) / TILE_V), n_rows = nm * 256;
   const int planes = (count + g.tile_rows - 1) / g.tile_rows * g.tile_rows / BK;      // of by_entry that exist
-  const int k_all = nv * (TILE_V / BK), k_slice = g.k_slice;
+  const int k_all = nv * (TILE_V / BK), k_slice = cut.slice * (TILE_V / BK);
   const int n_dh = g.dh32 ? (k_all + k_slice - 1) / k_slice * nm * nd : 0, n_dw = g.dw ? nv * nd : 0;
   // the item of a ticket: eighth x of both kinds; -1: none left there
   auto first_of = [](int n, int x) { return x * (n >> 3) + min(x, n & 7); };
@@ -347,15 +417,15 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(Head q, GradParams g) {
     if (i < n_dh) {
       const int dt = i % nd, rest = i / nd, mt = rest % nm, k0 = rest / nm * k_slice;
       c.kind = 0; c.row0 = mt * 256; c.col0 = dt * 256; c.ksteps = min(k_slice, k_all - k0);
-      const int v = g.v_begin + k0 * BK;
+      const int v = v_begin + k0 * BK;
       c.x = q.w + v * q.ldw + c.col0; c.ldx = q.ldw; c.x_rows = min(q.vocab - v, c.ksteps * BK);
-      c.w = g.by_row + (int64_t)k0 * (g.n_pad >> 5) * 2048; c.w_n = g.n_pad; c.w_planes = c.ksteps; c.w_row = c.row0;
+      c.w = g.by_row + (int64_t)k0 * (n_rows >> 5) * 2048; c.w_n = n_rows; c.w_planes = c.ksteps; c.w_row = c.row0;
       c.kind = rest / nm;
     } else {
       const int j = i - n_dh, dt = j % nd, vt = j / nd;
       c.kind = -1; c.row0 = vt * TILE_V; c.col0 = dt * 256; c.ksteps = max(4, (planes + 3) / 4 * 4);
       c.x = g.copy + c.col0; c.ldx = q.d; c.x_rows = g.n_pad;
-      c.w = g.by_entry; c.w_n = g.width; c.w_planes = planes; c.w_row = c.row0;
+      c.w = g.by_entry; c.w_n = cut.piece * TILE_V; c.w_planes = planes; c.w_row = c.row0;
     }
     return c;
   };
@@ -381,13 +451,13 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(Head q, GradParams g) {
     for (int b = 0; b < 2; ++b) {
       const int r = c.row0 + (t.wn * 2 + b) * 32 + t.lrow;
       if (c.kind >= 0) {
-        float *o = g.dh32 + ((int64_t)c.kind * g.n_pad + r) * q.d + c.col0 + t.half * 4;
+        float *o = g.dh32 + ((int64_t)c.kind * n_rows + r) * q.d + c.col0 + t.half * 4;
         if (r < count) {
 #pragma unroll
           for (int a = 0; a < 8; ++a) {
             f32x4 sum[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sum[i] = g.v_begin > 0 ? *(const f32x4 *)(o + a * 32 + i * 8) : f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int i = 0; i < 4; ++i) sum[i] = v_begin > 0 ? *(const f32x4 *)(o + a * 32 + i * 8) : f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < 4; ++i)
               *(f32x4 *)(o + a * 32 + i * 8) = sum[i] + f32x4{t.result(a, b, 4 * i), t.result(a, b, 4 * i + 1), t.result(a, b, 4 * i + 2), t.result(a, b, 4 * i + 3)};
@@ -397,7 +467,7 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(Head q, GradParams g) {
           }
         }
       } else {
-        bf16_t *o = g.dw + (int64_t)(g.v_begin + r) * q.d + c.col0 + t.half * 8;
+        bf16_t *o = g.dw + (int64_t)(v_begin + r) * q.d + c.col0 + t.half * 8;
 #pragma unroll
         for (int a = 0; a < 8; ++a) {
           float v[16];
@@ -405,7 +475,7 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(Head q, GradParams g) {
           for (int i = 0; i < 16; ++i) v[i] = t.result(a, b, i);
           uint4 f[2];
           fragments(f, v);
-          if (g.v_begin + r < q.vocab) {
+          if (v_begin + r < q.vocab) {
 #pragma unroll
             for (int k = 0; k < 2; ++k) *(uint4 *)(o + a * 32 + k * 16) = f[k];
           }
@@ -419,9 +489,12 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(Head q, GradParams g) {
 }
 
 // dh of every position: the slices of its row added up in order and rounded, or zeros
-__global__ __launch_bounds__(256) void loss_round_kernel(const float *__restrict__ dh32, bf16_t *__restrict__ dh, const int32_t *__restrict__ place, int slices, int n_pad, int d) {
+__global__ __launch_bounds__(256) void loss_round_kernel(const float *__restrict__ dh32, bf16_t *__restrict__ dh, const int32_t *__restrict__ place,
+                                                         const int32_t *__restrict__ count, int vocab, int d, int64_t ldw, int64_t most) {
   const int t = blockIdx.x, k = (blockIdx.y * 256 + threadIdx.x) * 4, r = place[t];
   if (k >= d) return;
+  const GradCut cut(*count, (vocab + TILE_V - 1) / TILE_V, d, ldw, most);
+  const int slices = cut.slices, n_pad = cut.nm * 256;
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
   if (r >= 0)
     for (int s = 0; s < slices; ++s) v += *(const f32x4 *)(dh32 + ((int64_t)s * n_pad + r) * d + k);
@@ -463,36 +536,44 @@ struct ForwardSpace {
   }
 };
 
-// Vocabulary entries of a piece of the gradient: G, both ways, in 256 MB (what the last-level cache holds), at least a tile, and W's part of it
-// behind a 32-bit offset.
-int grad_width(int n_pad, int vocab) {
-  return (int)std::max<int64_t>(1, std::min<int64_t>(((int64_t)vocab + 255) / 256, ((int64_t)64 << 20) / n_pad / 256)) * 256;
-}
-// Slices of dh along a piece's vocabulary: until there are as many tiles as units (each is 4 n d bytes, read and written per piece).
-int grad_slices(int n_pad, int width, int d) {
-  const int tiles = n_pad / 256 * (d / 256);
-  return std::max(1, std::min({UNITS / tiles, width / 1024, 16}));
-}
+// Elements of a piece's G, each way: both and the chunk of W that goes with them are read again soon.  (7B shape, 4096 positions: @MOST@.)
+constexpr int64_t GRAD_MOST = (int64_t)96 << 20;
+constexpr int NUMBER_MOST = 1024;   // positions that the gather's workgroups number for themselves
 
 struct GradSpace {
   int32_t *count, *tickets, *rows, *place;
   Row *info;
   bf16_t *op, *copy, *by_row, *by_entry;
   float *dh32;
-  int n_pad, width, slices;
+  int n_pad;
   int64_t bytes;
   GradSpace(void *ws, int n, int vocab, int d) {
     Carver c{(char *)ws};
     n_pad = padded(n);
-    width = grad_width(n_pad, vocab);
-    slices = grad_slices(n_pad, width, d);
+    // the most that any number of rows asks for
+    int64_t g = 0, sums = 0;
+    for (int rows = 256; rows <= n_pad; rows += 256) {
+      const GradCut cut(rows, (vocab + TILE_V - 1) / TILE_V, d, d, GRAD_MOST);
+      g = std::max(g, (int64_t)rows * cut.piece * TILE_V);
+      sums = std::max(sums, (int64_t)rows * cut.slices_most);
+    }
     count = c.take<int32_t>(1); tickets = c.take<int32_t>(8 * 32); rows = c.take<int32_t>(n); place = c.take<int32_t>(n); info = c.take<Row>(n_pad);
     op = c.take<bf16_t>((int64_t)n_pad * d); copy = c.take<bf16_t>((int64_t)n_pad * d);
-    by_row = c.take<bf16_t>((int64_t)n_pad * width); by_entry = c.take<bf16_t>((int64_t)n_pad * width);
-    dh32 = c.take<float>((int64_t)slices * n_pad * d);
+    by_row = c.take<bf16_t>(g); by_entry = c.take<bf16_t>(g);
+    dh32 = c.take<float>(sums * d);
     bytes = c.at - (char *)ws;
   }
 };
+// pieces that any number of rows asks for
+int grad_pieces(int n_pad, int vocab, int d, int64_t ldw) {
+  const int v_tiles = (vocab + TILE_V - 1) / TILE_V;
+  int most = 1;
+  for (int rows = 256; rows <= n_pad; rows += 256) {
+    const GradCut cut(rows, v_tiles, d, ldw, GRAD_MOST);
+    most = std::max(most, (v_tiles + cut.piece - 1) / cut.piece);
+  }
+  return most;
+}
 
 // calls f(rows of a tile, a kernel's shape as constants)
 template <typename F>
@@ -511,13 +592,18 @@ int64_t token_logprob_workspace_bytes(int n, int vocab, int d) { return ForwardS
 int launch_token_logprob(const TokenLoss &p, float *logprob, float *lse, hipStream_t s) {
   const ForwardSpace w(p.workspace, p.n, p.vocab, p.d);
   const Head q{p.h, p.w, p.ldh, p.ldw, p.target, p.inv_t, nullptr, nullptr, w.rows, w.count, p.vocab, p.d};
-  hipLaunchKernelGGL(loss_rows_kernel, dim3(1), dim3(1024), 0, s, p.target, w.count, w.rows, (int32_t *)nullptr, logprob, lse, p.n, p.vocab);
+  const Positions at{p.target, w.count, w.rows, nullptr, logprob, lse, p.n, p.vocab};
+  const bool number = p.n <= NUMBER_MOST;
+  if (!number) hipLaunchKernelGGL(loss_rows_kernel, dim3(1), dim3(1024), 0, s, at);
   for (int first = 0; first < p.n; first += PIECE) {
-    hipLaunchKernelGGL(loss_gather_kernel, dim3(w.n_pad / 32, p.d / 64), dim3(256), 0, s, q, first, w.op, (bf16_t *)nullptr, w.info);
+    auto gather = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(w.n_pad / 32, p.d / 64), dim3(256), 0, s, q, at, first, w.op, (bf16_t *)nullptr, w.info); };
+    if (number) gather(loss_gather_kernel<true>); else gather(loss_gather_kernel<false>);
     with_shape(std::min(p.n - first, PIECE), true, [&](auto WM, auto WN, auto AT, auto BT) {
-      hipLaunchKernelGGL((loss_forward_kernel<WM.value, WN.value, AT.value, BT.value>), dim3(UNITS), dim3(256), 0, s, q, w.op, w.info, w.parts, w.zt, first, w.n_pad);
+      auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(UNITS), dim3(256), 0, s, q, w.op, w.info, w.parts, w.zt, first, w.n_pad); };
+      constexpr bool once = WM.value > 1;   // (tiles of up to 128 rows: there is one of them)
+      launch(loss_forward_kernel<WM.value, WN.value, AT.value, BT.value, once>);
     });
-    hipLaunchKernelGGL(loss_merge_kernel, dim3(w.n_pad / 64), dim3(1024), 0, s, w.parts, w.zt, w.rows, w.count, logprob, lse, w.groups, first, w.n_pad);
+    hipLaunchKernelGGL(loss_merge_kernel, dim3(w.n_pad / 16), dim3(1024), 0, s, w.parts, w.zt, w.rows, w.count, logprob, lse, w.groups, first, w.n_pad);
   }
   return done();
 }
@@ -527,22 +613,22 @@ int64_t token_logprob_grad_workspace_bytes(int n, int vocab, int d) { return Gra
 int launch_token_logprob_grad(const TokenLoss &p, const float *lse, const float *g, bf16_t *dh, bf16_t *dw, hipStream_t s) {
   const GradSpace w(p.workspace, p.n, p.vocab, p.d);
   const Head q{p.h, p.w, p.ldh, p.ldw, p.target, p.inv_t, lse, g, w.rows, w.count, p.vocab, p.d};
-  hipLaunchKernelGGL(loss_rows_kernel, dim3(1), dim3(1024), 0, s, p.target, w.count, w.rows, w.place, (float *)nullptr, (float *)nullptr, p.n, p.vocab);
-  hipLaunchKernelGGL(loss_gather_kernel, dim3(w.n_pad / 32, p.d / 64), dim3(256), 0, s, q, 0, w.op, w.copy, w.info);
-  // (W's rows of a piece lie behind one 32-bit offset)
-  const int width = (int)std::min<int64_t>(w.width, (((int64_t)1 << 30) / p.ldw) / 256 * 256);
-  // tiles of a slice from the first piece, the largest: later ones have no slice that it has not
-  const int first_tiles = (std::min(width, p.vocab) + TILE_V - 1) / TILE_V, slice_tiles = (first_tiles + w.slices - 1) / w.slices;
+  const Positions at{p.target, w.count, w.rows, w.place, nullptr, nullptr, p.n, p.vocab};
+  const bool number = p.n <= NUMBER_MOST;
+  if (!number) hipLaunchKernelGGL(loss_rows_kernel, dim3(1), dim3(1024), 0, s, at);
+  auto gather = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(w.n_pad / 32, p.d / 64), dim3(256), 0, s, q, at, 0, w.op, w.copy, w.info); };
+  if (number) gather(loss_gather_kernel<true>); else gather(loss_gather_kernel<false>);
+  const int pieces = grad_pieces(w.n_pad, p.vocab, p.d, p.ldw);
   with_shape(p.n, false, [&](auto WM, auto WN, auto AT, auto BT) {
-    for (int v = 0; v < p.vocab; v += width) {
-      const int n_v = std::min(width, p.vocab - v);
+    for (int i = 0; i < pieces; ++i) {
       hipLaunchKernelGGL((loss_grad_logits_kernel<WM.value, WN.value, AT.value, BT.value>), dim3(UNITS), dim3(256), 0, s, q, w.op, w.info, dh ? w.by_row : nullptr,
-                         dw ? w.by_entry : nullptr, v, n_v, w.width, w.n_pad, w.tickets);
-      const GradParams gp{w.by_row, w.by_entry, w.copy, dh ? w.dh32 : nullptr, dw, w.tickets, v, n_v, w.width, w.n_pad, slice_tiles * (TILE_V / BK), WN.value * BT.value * 32};
+                         dw ? w.by_entry : nullptr, i, GRAD_MOST, w.n_pad, w.tickets);
+      const GradParams gp{w.by_row, w.by_entry, w.copy, dh ? w.dh32 : nullptr, dw, w.tickets, GRAD_MOST, i, w.n_pad, WN.value * BT.value * 32};
       hipLaunchKernelGGL(loss_grad_kernel, dim3(UNITS), dim3(256), 0, s, q, gp);
     }
   });
-  if (dh) hipLaunchKernelGGL(loss_round_kernel, dim3(p.n, (p.d / 4 + 255) / 256), dim3(256), 0, s, w.dh32, dh, w.place, (first_tiles + slice_tiles - 1) / slice_tiles, w.n_pad, p.d);
+  if (dh)
+    hipLaunchKernelGGL(loss_round_kernel, dim3(p.n, (p.d / 4 + 255) / 256), dim3(256), 0, s, w.dh32, dh, w.place, w.count, p.vocab, p.d, p.ldw, GRAD_MOST);
   return done();
 }
 
