@@ -45,8 +45,9 @@ constexpr int W_CACHE = WM == 1 && COLD ? 2 : 0;
 // TILE_COLS, x as the first operand, so that a lane ends with one column of W and groups of four consecutive rows of x;
 // TILE_COLS_T, the same with x k-major in memory (a row of it is one k): a k-step's 64 rows of BM lie in LDS as they come, and transposing reads
 // bring a lane its four k of one column, two reads per fragment.  Row k has its 16-byte chunks at slots chunk ^ 4 (k & 3), so that the four
-// k rows of a read lie in different banks.
-enum { TILE_ROWS, TILE_INT8, TILE_COLS, TILE_COLS_T };
+// k rows of a read lie in different banks; TILE_ROWS_T, W first again, with x an operand-ordered image taken across: the image's k are rows of x, its rows
+// are k.  LDS holds, for each chunk of eight rows of x, 64 k of 16 bytes, number m at slot m ^ 4 (chunk & 3), read by transposing too.
+enum { TILE_ROWS, TILE_INT8, TILE_COLS, TILE_COLS_T, TILE_ROWS_T };
 template <int WM, int WN, int AT, int BT, bool COLD, int KIND = TILE_ROWS>
 struct Tile {
   static constexpr int BM = WM * AT * 32, BN = WN * BT * 32;
@@ -55,7 +56,8 @@ struct Tile {
   static constexpr int X_CACHE = KIND == TILE_COLS && COLD ? 2 : 0;   // (weights are x there; non-temporal where nothing reads them again)
   // Offsets of x held per lane: one per load; of the kinds that address whole tiles, those that differ by more than a number of rows, which a scalar
   // adds (their kernels have no register to spare: a spill in the main loop waits for every load in flight).
-  static constexpr int XL = KIND == TILE_ROWS ? XI : KIND != TILE_COLS_T ? 1 : BM == 256 ? 2 : 1;
+  static constexpr int XL = KIND == TILE_ROWS ? XI : KIND == TILE_ROWS_T ? 4 : KIND == TILE_COLS_T && BM == 256 ? 2 : 1;
+  static constexpr bool TURNED = KIND == TILE_COLS_T || KIND == TILE_ROWS_T;   // two reads of LDS per fragment
   static_assert(WM * WN == 4 && BT <= 2, "tile");
 
   // where a tile's operands are
@@ -112,25 +114,35 @@ struct Tile {
       if constexpr (KIND == TILE_COLS_T) {   // (j: block of 32 rows of x, modulo 4)
         const int s = l & 15, chunk = wm * AT * 4 + j * 4 + ((l >> 4) & 1) * 2 + ((s & 3) >> 1);
         a_off[j] = (half * 32 + (s >> 2)) * BM + (chunk ^ (4 * (s >> 2))) * 8 + (s & 1) * 4;
+      } else if constexpr (KIND == TILE_ROWS_T) {   // (j: the k's bits 2 and 3)
+        const int s = l & 15, chunk = wm * AT * 4 + ((l >> 4) & 1) * 2 + ((s & 3) >> 1);
+        a_off[j] = (chunk * 64 + half * 32 + ((j * 4) ^ (4 * (chunk & 3))) + (s >> 2)) * 8 + (s & 1) * 4;
       } else {
         a_off[j] = (wm * AT * 32 + lrow) * BK + ((half * 4 + j) ^ (lrow & 7)) * 8;
       }
     }
   }
-  // x: rows (TILE_COLS_T: k) ldx elements apart from X on, of which `rows` exist (further ones read as 0);
+  // x: rows (TILE_COLS_T: k) ldx elements apart from X on, of which `rows` exist (further ones read as 0); TILE_ROWS_T: an image of ldx rows, from the plane at
+  // X on, of which `rows` planes of 64 exist;
   // w: operand-ordered, `n` of its rows per plane and `planes` k-steps from W on (further ones read as 0), the tile's from w_row on.
   __device__ __forceinline__ Part part_at(const bf16_t *X, int64_t ldx, int rows, const bf16_t *W, int n, int planes, int w_row) {
     Part p;
     w_plane = (uint32_t)(n >> 5) * 4096u;
     rw = __builtin_amdgcn_make_buffer_rsrc((void *)W, 0, (int)((uint32_t)planes * w_plane), 0x00020000);
-    const int64_t x_bytes = (int64_t)rows * ldx * 2;
+    const int64_t x_bytes = (int64_t)rows * ldx * (KIND == TILE_ROWS_T ? 128 : 2);
     rx = __builtin_amdgcn_make_buffer_rsrc((void *)X, 0, (int)min(x_bytes, (int64_t)0x7fffffff), 0x00020000);
     constexpr int PER = KIND == TILE_COLS_T ? BM / 8 : BK / 8, ROWS = 64 / PER;   // chunks of a row (of 64 k or of BM columns), rows of a load
     static_assert(KIND != TILE_COLS_T || ROWS * XL == 4, "the slots of a row go by its number modulo 4");
-    x_step = KIND == TILE_COLS_T ? (int)(BK * 2 * ldx) : BK * 2;
-    x_load = (int)(ROWS * 2 * ldx);
+    static_assert(KIND != TILE_ROWS_T || XI == 8, "a wavefront loads a plane's part of a k-step");
+    x_step = KIND == TILE_COLS_T ? (int)(BK * 2 * ldx) : KIND == TILE_ROWS_T ? 2 * 4096 : BK * 2;
+    x_load = KIND == TILE_ROWS_T ? (int)(ldx * 128) : (int)(ROWS * 2 * ldx);   // (TILE_ROWS_T: from a plane to the next)
 #pragma unroll
     for (int i = 0; i < XL; ++i) {
+      if constexpr (KIND == TILE_ROWS_T) {
+        const int m = l ^ (4 * i);
+        p.x_lane[i] = (m >> 5) * 4096 + (m & 31) * 16;
+        continue;
+      }
       const int k = l / PER;
       p.x_lane[i] = (int)(k * ldx * 2) + ((l % PER) ^ (KIND == TILE_COLS_T ? 4 * ((i * ROWS + k) & 3) : l / PER)) * 16;
     }
@@ -152,7 +164,10 @@ struct Tile {
 #pragma unroll
     for (int i = i0; i < i1; ++i)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (lds_void *)(xs + st * STAGE + (wave * XI + i) * 512), 16, p.x_lane[i % XL],
-                                               KIND == TILE_ROWS ? p.x_k + ks * (BK * 2) : ks * x_step + (wave * XI + i) * x_load, 0, X_CACHE);
+                                               KIND == TILE_ROWS     ? p.x_k + ks * (BK * 2)
+                                               : KIND == TILE_ROWS_T ? ks * x_step + wave * x_load + (i & 3) * 1024 + (i >> 2) * 512
+                                                                     : ks * x_step + (wave * XI + i) * x_load,
+                                               0, X_CACHE);
 #endif
   }
   __device__ __forceinline__ void load_w(const Part &p, int st, int ks, int b) {
@@ -169,10 +184,17 @@ struct Tile {
   __device__ __forceinline__ void read_a(int st, int j) {
 #pragma unroll
     for (int a = 0; a < AT; ++a) {
-      if constexpr (KIND == TILE_COLS_T) {
+      if constexpr (TURNED) {
 #ifdef __HIP_DEVICE_COMPILE__
-        bf16_t *at = xs + st * STAGE + a_off[a & 3] + (a >> 2) * 128 + j * 8 * BM;
-        const s16x4 lo = read_transposed((lds_s16x4 *)at), hi = read_transposed((lds_s16x4 *)(at + 4 * BM));
+        bf16_t *at = xs + st * STAGE, *at_lo, *at_hi;
+        if constexpr (KIND == TILE_COLS_T) {
+          at_lo = at + a_off[a & 3] + (a >> 2) * 128 + j * 8 * BM;
+          at_hi = at_lo + 4 * BM;
+        } else {
+          at_lo = at + a_off[(j & 1) * 2] + (j >> 1) * 128 + a * 2048;
+          at_hi = at + a_off[(j & 1) * 2 + 1] + (j >> 1) * 128 + a * 2048;
+        }
+        const s16x4 lo = read_transposed((lds_s16x4 *)at_lo), hi = read_transposed((lds_s16x4 *)at_hi);
         af[j & 1][a] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 #endif
       } else {
@@ -188,7 +210,7 @@ struct Tile {
 #ifdef __HIP_DEVICE_COMPILE__
         if constexpr (KIND == TILE_INT8)
           acc[a][b] = __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4, wf[st][b][j]), __builtin_bit_cast(i32x4, af[j & 1][a]), acc[a][b], 0, 0, 0);
-        else if constexpr (KIND == TILE_ROWS)
+        else if constexpr (KIND == TILE_ROWS || KIND == TILE_ROWS_T)
           acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wf[st][b][j], af[j & 1][a], acc[a][b], 0, 0, 0);
         else
           acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(af[j & 1][a], wf[st][b][j], acc[a][b], 0, 0, 0);
@@ -232,7 +254,7 @@ struct Tile {
     constexpr int per = VM >= AT ? VM / AT : 1;
 #pragma unroll
     for (int i = 0; i < AT; ++i) {
-      if (READS) __builtin_amdgcn_sched_group_barrier(0x100, KIND == TILE_COLS_T ? 2 : 1, 0);
+      if (READS) __builtin_amdgcn_sched_group_barrier(0x100, TURNED ? 2 : 1, 0);
       __builtin_amdgcn_sched_group_barrier(0x008, BT, 0);
       if (VM >= AT || i * VM / AT != (i + 1) * VM / AT) __builtin_amdgcn_sched_group_barrier(0x020, per, 0);
     }
@@ -274,7 +296,7 @@ struct Tile {
 #pragma unroll
       for (int i = 0; i < AT; ++i) {
         __builtin_amdgcn_sched_group_barrier(0x008, BT, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, KIND == TILE_COLS_T ? 2 : 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, TURNED ? 2 : 1, 0);
         if (LOAD && BT > 1 && (4 >= AT || i * 4 / AT != (i + 1) * 4 / AT)) __builtin_amdgcn_sched_group_barrier(0x020, 4 >= AT ? 4 / AT : 1, 0);
       }
     }
@@ -424,10 +446,10 @@ __device__ __forceinline__ void one_tile(T &t, const Item &c) {
 }
 
 // Tiles one after the other, the next one's first k-steps under the last products of the one at hand.  take(item): the next tile, or false; a tile is
-// known one tile ahead, and ask() is called as a tile begins, in time for the take() behind it.  One loop of four k-steps for all of a tile: with last k-steps
+// known one tile ahead; ask() is called as a tile begins and told() near its end, with barriers between it and the take() behind it.  One loop of four k-steps for all of a tile: with last k-steps
 // of their own, behind the loop, the accumulators move between the two, and what spills meanwhile waits for every load in flight.
-template <typename T, typename Ask, typename Take, typename Done>
-__device__ __forceinline__ void walk(T &t, Ask ask, Take take, Done done) {
+template <typename T, typename Ask, typename Told, typename Take, typename Done>
+__device__ __forceinline__ void walk(T &t, Ask ask, Told told, Take take, Done done) {
   Item c, d;
   if (!take(c)) return;
   d = c;   // behind the last tile: its own first k-steps again, which nothing reads
@@ -445,6 +467,7 @@ __device__ __forceinline__ void walk(T &t, Ask ask, Take take, Done done) {
         p = part_of(t, d);
         at = 0;
         ks = -1;
+        told();
       }
       t.template kstep<1, true, 3>(p, at);
       t.template kstep<2, true, 3>(p, at + 1);

@@ -265,7 +265,7 @@ __global__ __launch_bounds__(256) void gemm_int8_rounds_kernel(Int8Params g) {
   at += blockIdx.x >> 3;
   T t;
   t.init_at(xs);
-  walk(t, [] {}, [&](Item &d) {
+  walk(t, [] {}, [] {}, [&](Item &d) {
     if (at >= end) return false;
     d = int8_item<T>(g, at % g.nrow, at / g.nrow, 0);
     at += gridDim.x >> 3;

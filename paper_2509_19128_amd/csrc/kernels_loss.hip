@@ -3,13 +3,12 @@
 //   z[t, v] = inv_t[t] * sum_k h[t, k] W[v, k],  lse[t] = log sum_v exp z[t, v],  logprob[t] = z[t, y_t] - lse[t]
 //   G[t, v] = g[t] inv_t[t] (1[v = y_t] - exp(z[t, v] - lse[t])),  dh = G W,  dW = G^T h
 //
-// Four products on the matrix cores, all by the tiles of gemm_tile.h with x as the first operand, so that a lane ends with one column and
-// many rows:
+// Four products on the matrix cores, by the tiles of gemm_tile.h:
 //   logits (forward, and again for the gradient)   x = W (rows v), w = h               a lane ends with one position and its logits
 //   dh                                             x = W, k-major (rows d, k = v), w = G   a lane ends with one position and columns of dh
-//   dW                                             x = h, k-major (rows d, k = t), w = G^T a lane ends with one vocabulary entry
-// so W is read as it lies (row-major, no transposed copy), and what is reordered is small: h once per call, G where it is made.  A position's
-// maximum and sum of exponentials are then sums over a lane's registers and one swap of halves.
+//   dW                                             x = G, across (rows v, k = t), w = h^T  a lane ends with one vocabulary entry
+// so W is read as it lies (row-major, no transposed copy), G is written once, in operand order, and what else is reordered is small: h and h^T, once per
+// call.  A position's maximum and sum of exponentials are then sums over a lane's registers and one swap of halves.
 //
 // Positions without a target are left out from the start: the others are numbered, gathered and padded with zeros to whole tiles, and every
 // kernel works on those ("rows" below); how many there are is known on the device only.
@@ -79,10 +78,10 @@ struct Head {
   int vocab, d;
 };
 
-// Rows [first, first + 32 * gridDim.x) in operand order (planes of 64 k, blocks of 32 rows; padding 0), as they are (copy, if any), and what
-// the tiles want to know of each.  NUMBER: few positions, which every workgroup numbers for itself instead of a launch ahead.
+// Rows [first, first + 32 * gridDim.x) in operand order (planes of 64 k, blocks of 32 rows; padding 0), their transpose in operand order (if any: planes
+// of 64 rows, blocks of 32 k), and what the tiles want to know of each.  NUMBER: few positions, which every workgroup numbers for itself instead of a launch ahead.
 template <bool NUMBER>
-__global__ __launch_bounds__(256) void loss_gather_kernel(Head q, Positions at, int first, bf16_t *__restrict__ op, bf16_t *__restrict__ copy, Row *__restrict__ info) {
+__global__ __launch_bounds__(256) void loss_gather_kernel(Head q, Positions at, int first, bf16_t *__restrict__ op, bf16_t *__restrict__ turned, Row *__restrict__ info) {
   const int r0 = blockIdx.x * 32, j = threadIdx.x >> 6, half = (threadIdx.x >> 5) & 1, r = r0 + (threadIdx.x & 31), k = blockIdx.y * 64 + half * 32 + j * 8;
   int t = -1;
   if constexpr (NUMBER) {
@@ -101,7 +100,17 @@ __global__ __launch_bounds__(256) void loss_gather_kernel(Head q, Positions at, 
   }
   const uint4 v = t >= 0 ? *(const uint4 *)(q.h + t * q.ldh + k) : make_uint4(0, 0, 0, 0);
   *(uint4 *)(op + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 2048 + threadIdx.x * 8) = v;
-  if (copy) *(uint4 *)(copy + (int64_t)r * q.d + k) = v;
+  if (turned) {   // (uniform)
+    __shared__ __attribute__((aligned(16))) bf16_t block[32][72];
+    *(uint4 *)&block[threadIdx.x & 31][half * 32 + j * 8] = v;
+    __syncthreads();
+    const int c = threadIdx.x & 63;   // column, and eight rows from j * 8 on
+    bf16x8 o;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = block[j * 8 + e][c];
+    const int k32 = (blockIdx.y * 64 + c) >> 5;
+    *(bf16x8 *)(turned + ((((int64_t)(r0 >> 6) * (q.d >> 5) + k32) * 4 + j) * 64 + ((r0 >> 5) & 1) * 32 + (c & 31)) * 8) = o;
+  }
   if (blockIdx.y == 0 && threadIdx.x < 32) {
     Row i{0.f, 0.f, 0.f, -1};
     if (t >= 0) {
@@ -156,7 +165,7 @@ __global__ __launch_bounds__(256) void loss_forward_kernel(Head q, const bf16_t 
   if (tiles.at >= tiles.end) return;
   T t;
   t.init_at(xs);
-  walk(t, [] {}, [&](Item &d) {
+  walk(t, [] {}, [] {}, [&](Item &d) {
     if (tiles.at >= tiles.end) return false;
     int mt, vt;
     tiles.place(mt, vt);
@@ -273,7 +282,7 @@ __device__ __forceinline__ int64_t fragment_place(int row, int k32, int n, int f
 }
 
 // How the gradient is cut, from the number of rows, which the device knows: vocabulary tiles of a piece, tiles of a slice of dh along a piece, and slices.
-// A piece's G, both ways, takes at most `most` elements each (or one vocabulary tile's); its tiles of 256 rows are whole rounds of the units where there
+// A piece's G takes at most `most` elements (or one vocabulary tile's); its tiles of 256 rows are whole rounds of the units where there
 // are that many.  Slices of dh: until there are as many tiles as units (each is a sum of its own that is read and written per piece).
 struct GradCut {
   int nm, piece, slice, slices, slices_most;   // (slices_most: of any piece of this many rows)
@@ -293,26 +302,24 @@ struct GradCut {
   }
 };
 
-// G of vocabulary entries [v_begin, v_begin + n_v), in operand order both ways: `by_row` for dh (a row's entries are its k) and `by_entry` for dW (an entry's
-// rows are its k).  The second is the first's transpose by the matrix cores: a product with the unit matrix moves what a lane holds of a position
-// to the lane of the entry, exactly.  Clears the tickets of the kernel behind.
+// G of a piece of the vocabulary, in operand order (a row's entries are its k; rows to whole tiles).  Clears the tickets of the kernel behind.
 template <int WM, int WN, int AT, int BT>
-__global__ __launch_bounds__(256) void loss_grad_logits_kernel(Head q, const bf16_t *__restrict__ op, const Row *__restrict__ info, bf16_t *__restrict__ by_row, bf16_t *__restrict__ by_entry,
+__global__ __launch_bounds__(256) void loss_grad_logits_kernel(Head q, const bf16_t *__restrict__ op, const Row *__restrict__ info, bf16_t *__restrict__ G_out,
                                                                int index, int64_t most, int n_pad, int32_t *__restrict__ tickets) {
   typedef Tile<WM, WN, AT, BT, false, TILE_COLS> T;
   __shared__ __attribute__((aligned(1024))) bf16_t xs[T::LDS];
-  if (blockIdx.x == 0 && threadIdx.x < 8) tickets[threadIdx.x * 32] = 0;
+  if (blockIdx.x == 0 && threadIdx.x < 16) tickets[threadIdx.x * 32] = 0;
   const int count = *q.count;
   const GradCut cut(count, (q.vocab + TILE_V - 1) / TILE_V, q.d, q.ldw, most);
   const int64_t begin = (int64_t)index * cut.piece * TILE_V;
   if (begin >= q.vocab) return;
-  const int v_begin = (int)begin, width = cut.piece * TILE_V, n_rows = cut.nm * 256;
+  const int v_begin = (int)begin, width = cut.piece * TILE_V, n_rows = (count + T::BN - 1) / T::BN * T::BN;
   LogitTiles<T::BN> tiles;
   tiles.init(count, min(width, q.vocab - v_begin));
   if (tiles.at >= tiles.end) return;
   T t;
   t.init_at(xs);
-  walk(t, [] {}, [&](Item &d) {
+  walk(t, [] {}, [] {}, [&](Item &d) {
     if (tiles.at >= tiles.end) return false;
     int mt, vt;
     tiles.place(mt, vt);
@@ -321,11 +328,6 @@ __global__ __launch_bounds__(256) void loss_grad_logits_kernel(Head q, const bf1
     return true;
   }, [&](const Item &c) {
     const int v0 = c.col0 + t.wm * AT * 32;
-    bf16x8 unit[2];
-#pragma unroll
-    for (int f = 0; f < 2; ++f)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) unit[f][e] = (bf16_t)(t.lrow - t.half * 8 == f * 16 + e ? 1.f : 0.f);
 #pragma unroll
     for (int b = 0; b < BT; ++b) {
       const int m32 = (c.row0 >> 5) + t.wn * BT + b;
@@ -348,25 +350,8 @@ __global__ __launch_bounds__(256) void loss_grad_logits_kernel(Head q, const bf1
         }
         uint4 f[2];
         fragments(f, G);
-        if (by_row) {
 #pragma unroll
-          for (int k = 0; k < 2; ++k) *(uint4 *)((char *)by_row + fragment_place(m32, v32, n_rows, k, t.half, t.lrow)) = f[k];
-        }
-        if (by_entry) {
-          f32x16 turned;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) turned[i] = 0.f;
-#ifdef __HIP_DEVICE_COMPILE__
-#pragma unroll
-          for (int k = 0; k < 2; ++k) turned = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f[k]), unit[k], turned, 0, 0, 0);
-#endif
-          float G2[16];
-#pragma unroll
-          for (int i = 0; i < 16; ++i) G2[i] = turned[i];
-          fragments(f, G2);
-#pragma unroll
-          for (int k = 0; k < 2; ++k) *(uint4 *)((char *)by_entry + fragment_place(v32, m32, width, k, t.half, t.lrow)) = f[k];
-        }
+        for (int k = 0; k < 2; ++k) *(uint4 *)((char *)G_out + fragment_place(m32, v32, n_rows, k, t.half, t.lrow)) = f[k];
 #ifdef __HIP_DEVICE_COMPILE__
         __builtin_amdgcn_sched_barrier(0);   // (one block's registers at a time)
 #endif
@@ -376,81 +361,119 @@ __global__ __launch_bounds__(256) void loss_grad_logits_kernel(Head q, const bf1
 }
 
 struct GradParams {
-  const bf16_t *by_row, *by_entry, *copy;   // G both ways, h's rows
+  const bf16_t *G, *turned;                 // G in operand order, h^T in operand order
   float *dh32;                              // [slices][rows, to a multiple of 256][d], or null: no dh
   bf16_t *dw;                               // or null
-  int32_t *tickets;                         // eight, 128 bytes apart, zero
+  int32_t *tickets;                         // sixteen, 128 bytes apart, zero: eight of each kind of tile
   int64_t most;
-  int index, n_pad, tile_rows;              // the piece; rows of `copy`; rows of a tile of the kernel that made G (beyond its last tile there is nothing)
+  int index, n_pad, tile_rows;              // the piece; rows of `turned`; rows of a tile of the kernel that made G
 };
 
-// dh += G W and dW = G^T h of a piece of the vocabulary, 256 x 256 tiles of both in one launch: the units take them by tickets, those of dh, which
-// are the longer ones, first, from their own XCD's eighth of each kind, then from the others'.
+// Tiles that the units take by tickets, from their own XCD's eighth and, when that is done, from the others'.  One thread draws; the others read what it
+// leaves in LDS.  A ticket is asked for as a tile begins and looked at when the tile is nearly done.
+struct Lottery {
+  int32_t *tickets;   // eight, 128 bytes apart
+  int n, dealt, asked, from;
+  bool own;           // tickets of this XCD's eighth may be left
+  // dealt: so many of each eighth go one to each unit, without a ticket (tiles of which a unit is to take no second one while another has none)
+  __device__ __forceinline__ Lottery(int32_t *t, int n_, int dealt_) : tickets(t), n(n_), dealt(dealt_), asked(0), from(0), own(true) {}
+  __device__ __forceinline__ int first(int x) const { return x * (n >> 3) + min(x, n & 7); }
+  __device__ __forceinline__ int size(int x) const { return first(x + 1) - first(x); }
+  __device__ __forceinline__ int draw(int x) const {
+    return size(x) <= dealt ? size(x) : dealt + __hip_atomic_fetch_add(&tickets[x * 32], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  // a tile of another eighth, or -1: an eighth that looks unfinished is asked, and one that was finished meanwhile looks so the next time
+  __device__ __forceinline__ int steal() const {
+    for (;;) {
+      int seen[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) seen[k] = __hip_atomic_load(&tickets[((blockIdx.x + k) & 7) * 32], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      int x = -1;
+#pragma unroll
+      for (int k = 7; k >= 0; --k) {
+        const int y = (blockIdx.x + k) & 7;
+        if (dealt + seen[k] < size(y)) x = y;
+      }
+      if (x < 0) return -1;
+      const int i = draw(x);
+      if (i < size(x)) return first(x) + i;
+    }
+  }
+  // the first two tiles
+  template <typename Place>
+  __device__ __forceinline__ void begin(Place place) {
+    const int x = blockIdx.x & 7;
+    from = first(x);
+    int a = -1;
+    if ((int)(blockIdx.x >> 3) < min(dealt, size(x))) a = from + (blockIdx.x >> 3);
+    else if (dealt == 0) {
+      ask();
+      a = told();
+    }
+    place(0, a);
+    ask();
+    place(1, a < 0 ? -1 : told());
+  }
+  __device__ __forceinline__ void ask() {
+    if (own) asked = draw(blockIdx.x & 7);
+  }
+  __device__ __forceinline__ int told() {
+    if (own && asked < size(blockIdx.x & 7)) return from + asked;
+    own = false;
+    return steal();
+  }
+};
+
+// dh += G W and dW = G^T h of a piece of the vocabulary, 256 x 256 tiles, in one launch: first those of dh, which are the longer ones, then those of dW.
 __global__ __launch_bounds__(256) void loss_grad_kernel(Head q, GradParams g) {
-  typedef Tile<1, 4, 8, 2, false, TILE_COLS_T> T;
+  typedef Tile<1, 4, 8, 2, false, TILE_COLS_T> TH;
+  typedef Tile<1, 4, 8, 2, false, TILE_ROWS_T> TW;
   // (one LDS object: of two the compiler would know that loads on their way to one may not be what a read of it wants, and wait for them all)
-  __shared__ __attribute__((aligned(1024))) bf16_t xs[T::LDS + 4];
+  __shared__ __attribute__((aligned(1024))) bf16_t xs[TH::LDS + 4];
   typedef __attribute__((address_space(3))) volatile int32_t lds_int;
-  lds_int *drawn = (lds_int *)(xs + T::LDS);
+  lds_int *drawn = (lds_int *)(xs + TH::LDS);
   const int count = *q.count, nd = q.d / 256;
   const GradCut cut(count, (q.vocab + TILE_V - 1) / TILE_V, q.d, q.ldw, g.most);
   const int64_t begin = (int64_t)g.index * cut.piece * TILE_V;
   if (begin >= q.vocab) return;
   const int v_begin = (int)begin, nm = cut.nm, nv = min(cut.piece, (q.vocab - v_begin + TILE_V - 1) / TILE_V), n_rows = nm * 256;
-  const int planes = (count + g.tile_rows - 1) / g.tile_rows * g.tile_rows / BK;      // of by_entry that exist
+  const int g_rows = (count + g.tile_rows - 1) / g.tile_rows * g.tile_rows;   // of G
+  const int64_t g_plane = (int64_t)g_rows * 64;
   const int k_all = nv * (TILE_V / BK), k_slice = cut.slice * (TILE_V / BK);
-  const int n_dh = g.dh32 ? (k_all + k_slice - 1) / k_slice * nm * nd : 0, n_dw = g.dw ? nv * nd : 0;
-  // the item of a ticket: eighth x of both kinds; -1: none left there
-  auto first_of = [](int n, int x) { return x * (n >> 3) + min(x, n & 7); };
-  auto draw = [&]() {   // one thread
-    for (int k = 0; k < 8; ++k) {
-      const int x = (blockIdx.x + k) & 7, a = first_of(n_dh, x), n_a = first_of(n_dh, x + 1) - a, b = first_of(n_dw, x), n_b = first_of(n_dw, x + 1) - b;
-      if (n_a + n_b == 0) continue;
-      const int i = __hip_atomic_fetch_add(&g.tickets[x * 32], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      if (i < n_a) return a + i;
-      if (i < n_a + n_b) return n_dh + b + (i - n_a);
-    }
-    return -1;
+  // the walk over one kind of tile
+  auto tiles = [&](auto &t, int n, int dealt, int32_t *tickets, auto item, auto done) {
+    Lottery lots(tickets, n, dealt);
+    const bool draws = threadIdx.x == 0;
+    if (draws) lots.begin([&](int i, int v) { drawn[i] = v; });
+    __syncthreads();
+    t.init_at(xs);
+    int turn = 0;
+    walk(t, [&] {
+      if (draws) lots.ask();
+    }, [&] {
+      if (draws) drawn[turn] = lots.told();   // for the tile behind the next; this place was read a tile ago
+    }, [&](Item &d) {
+      const int i = __builtin_amdgcn_readfirstlane(drawn[turn]);
+      turn ^= 1;
+      if (i < 0) return false;
+      d = item(i);
+      return true;
+    }, done);
+    __syncthreads();
   };
-  auto item = [&](int i) {
-    Item c;
-    if (i < n_dh) {
-      const int dt = i % nd, rest = i / nd, mt = rest % nm, k0 = rest / nm * k_slice;
-      c.kind = 0; c.row0 = mt * 256; c.col0 = dt * 256; c.ksteps = min(k_slice, k_all - k0);
-      const int v = v_begin + k0 * BK;
+  if (g.dh32 && nm > 0) {
+    TH t;
+    tiles(t, (k_all + k_slice - 1) / k_slice * nm * nd, UNITS / 8, g.tickets, [&](int i) {
+      Item c;
+      const int dt = i % nd, rest = i / nd, mt = rest % nm, k0 = rest / nm * k_slice, v = v_begin + k0 * BK;
+      c.kind = rest / nm; c.row0 = mt * 256; c.col0 = dt * 256; c.ksteps = min(k_slice, k_all - k0);
       c.x = q.w + v * q.ldw + c.col0; c.ldx = q.ldw; c.x_rows = min(q.vocab - v, c.ksteps * BK);
-      c.w = g.by_row + (int64_t)k0 * (n_rows >> 5) * 2048; c.w_n = n_rows; c.w_planes = c.ksteps; c.w_row = c.row0;
-      c.kind = rest / nm;
-    } else {
-      const int j = i - n_dh, dt = j % nd, vt = j / nd;
-      c.kind = -1; c.row0 = vt * TILE_V; c.col0 = dt * 256; c.ksteps = max(4, (planes + 3) / 4 * 4);
-      c.x = g.copy + c.col0; c.ldx = q.d; c.x_rows = g.n_pad;
-      c.w = g.by_entry; c.w_n = cut.piece * TILE_V; c.w_planes = planes; c.w_row = c.row0;
-    }
-    return c;
-  };
-  if (threadIdx.x == 0) {
-    drawn[0] = draw();
-    drawn[1] = draw();
-  }
-  __syncthreads();
-  if (drawn[0] < 0) return;
-  T t;
-  t.init_at(xs);
-  int turn = 0;
-  walk(t, [&] {
-    if (threadIdx.x == 0) drawn[turn] = draw();   // for the tile behind the next: its place was read a tile ago, and is read again behind this tile's barriers
-  }, [&](Item &d) {
-    const int i = __builtin_amdgcn_readfirstlane(drawn[turn]);
-    turn ^= 1;
-    if (i < 0) return false;
-    d = item(i);
-    return true;
-  }, [&](const Item &c) {
+      c.w = g.G + k0 * g_plane; c.w_n = g_rows; c.w_planes = c.ksteps; c.w_row = c.row0;
+      return c;
+    }, [&](const Item &c) {
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const int r = c.row0 + (t.wn * 2 + b) * 32 + t.lrow;
-      if (c.kind >= 0) {
+      for (int b = 0; b < 2; ++b) {
+        const int r = c.row0 + (t.wn * 2 + b) * 32 + t.lrow;
         float *o = g.dh32 + ((int64_t)c.kind * n_rows + r) * q.d + c.col0 + t.half * 4;
         if (r < count) {
 #pragma unroll
@@ -466,26 +489,42 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(Head q, GradParams g) {
 #endif
           }
         }
-      } else {
-        bf16_t *o = g.dw + (int64_t)(v_begin + r) * q.d + c.col0 + t.half * 8;
+      }
+    });
+  }
+  if (g.dw) {
+    // G's rows behind its last tile do not exist: the last k-steps take other entries' rows in their place, against zeros of h^T
+    TW t;
+    tiles(t, nv * nd, 0, g.tickets + 8 * 32, [&](int i) {
+      Item c;
+      const int dt = i % nd, vt = i / nd;
+      c.kind = 0; c.row0 = vt * TILE_V; c.col0 = dt * 256; c.ksteps = max(4, (g_rows / BK + 3) / 4 * 4);
+      c.x = g.G + vt * 4 * g_plane; c.ldx = g_rows; c.x_rows = (nv - vt) * 4;
+      c.w = g.turned; c.w_n = q.d; c.w_planes = g_rows / BK; c.w_row = c.col0;
+      return c;
+    }, [&](const Item &c) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
 #pragma unroll
         for (int a = 0; a < 8; ++a) {
-          float v[16];
+          const int v = v_begin + c.row0 + a * 32 + t.lrow;
+          float s[16];
 #pragma unroll
-          for (int i = 0; i < 16; ++i) v[i] = t.result(a, b, i);
+          for (int i = 0; i < 16; ++i) s[i] = t.result(a, b, i);
           uint4 f[2];
-          fragments(f, v);
-          if (v_begin + r < q.vocab) {
+          fragments(f, s);
+          bf16_t *o = g.dw + (int64_t)v * q.d + c.col0 + (t.wn * 2 + b) * 32 + t.half * 8;
+          if (v < q.vocab) {
 #pragma unroll
-            for (int k = 0; k < 2; ++k) *(uint4 *)(o + a * 32 + k * 16) = f[k];
+            for (int k = 0; k < 2; ++k) *(uint4 *)(o + k * 16) = f[k];
           }
 #ifdef __HIP_DEVICE_COMPILE__
           __builtin_amdgcn_sched_barrier(0);   // (one block's registers at a time)
 #endif
         }
       }
-    }
-  });
+    });
+  }
 }
 
 // dh of every position: the slices of its row added up in order and rounded, or zeros
@@ -536,14 +575,14 @@ struct ForwardSpace {
   }
 };
 
-// Elements of a piece's G, each way: both and the chunk of W that goes with them are read again soon.  (7B shape, 4096 positions: @MOST@.)
+// Elements of a piece's G.  (7B shape, 4096 positions: @MOST@.)
 constexpr int64_t GRAD_MOST = (int64_t)96 << 20;
 constexpr int NUMBER_MOST = 1024;   // positions that the gather's workgroups number for themselves
 
 struct GradSpace {
   int32_t *count, *tickets, *rows, *place;
   Row *info;
-  bf16_t *op, *copy, *by_row, *by_entry;
+  bf16_t *op, *turned, *G;
   float *dh32;
   int n_pad;
   int64_t bytes;
@@ -557,9 +596,9 @@ struct GradSpace {
       g = std::max(g, (int64_t)rows * cut.piece * TILE_V);
       sums = std::max(sums, (int64_t)rows * cut.slices_most);
     }
-    count = c.take<int32_t>(1); tickets = c.take<int32_t>(8 * 32); rows = c.take<int32_t>(n); place = c.take<int32_t>(n); info = c.take<Row>(n_pad);
-    op = c.take<bf16_t>((int64_t)n_pad * d); copy = c.take<bf16_t>((int64_t)n_pad * d);
-    by_row = c.take<bf16_t>(g); by_entry = c.take<bf16_t>(g);
+    count = c.take<int32_t>(1); tickets = c.take<int32_t>(16 * 32); rows = c.take<int32_t>(n); place = c.take<int32_t>(n); info = c.take<Row>(n_pad);
+    op = c.take<bf16_t>((int64_t)n_pad * d); turned = c.take<bf16_t>((int64_t)n_pad * d);
+    G = c.take<bf16_t>(g);
     dh32 = c.take<float>(sums * d);
     bytes = c.at - (char *)ws;
   }
@@ -616,14 +655,14 @@ int launch_token_logprob_grad(const TokenLoss &p, const float *lse, const float 
   const Positions at{p.target, w.count, w.rows, w.place, nullptr, nullptr, p.n, p.vocab};
   const bool number = p.n <= NUMBER_MOST;
   if (!number) hipLaunchKernelGGL(loss_rows_kernel, dim3(1), dim3(1024), 0, s, at);
-  auto gather = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(w.n_pad / 32, p.d / 64), dim3(256), 0, s, q, at, 0, w.op, w.copy, w.info); };
+  auto gather = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(w.n_pad / 32, p.d / 64), dim3(256), 0, s, q, at, 0, w.op, w.turned, w.info); };
   if (number) gather(loss_gather_kernel<true>); else gather(loss_gather_kernel<false>);
   const int pieces = grad_pieces(w.n_pad, p.vocab, p.d, p.ldw);
   with_shape(p.n, false, [&](auto WM, auto WN, auto AT, auto BT) {
     for (int i = 0; i < pieces; ++i) {
-      hipLaunchKernelGGL((loss_grad_logits_kernel<WM.value, WN.value, AT.value, BT.value>), dim3(UNITS), dim3(256), 0, s, q, w.op, w.info, dh ? w.by_row : nullptr,
-                         dw ? w.by_entry : nullptr, i, GRAD_MOST, w.n_pad, w.tickets);
-      const GradParams gp{w.by_row, w.by_entry, w.copy, dh ? w.dh32 : nullptr, dw, w.tickets, GRAD_MOST, i, w.n_pad, WN.value * BT.value * 32};
+      hipLaunchKernelGGL((loss_grad_logits_kernel<WM.value, WN.value, AT.value, BT.value>), dim3(UNITS), dim3(256), 0, s, q, w.op, w.info, w.G, i, GRAD_MOST,
+                         w.n_pad, w.tickets);
+      const GradParams gp{w.G, w.turned, dh ? w.dh32 : nullptr, dw, w.tickets, GRAD_MOST, i, w.n_pad, WN.value * BT.value * 32};
       hipLaunchKernelGGL(loss_grad_kernel, dim3(UNITS), dim3(256), 0, s, q, gp);
     }
   });
