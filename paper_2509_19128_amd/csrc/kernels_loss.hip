@@ -20,12 +20,13 @@ namespace pl {
 namespace {
 
 constexpr int GROUP = 64;           // vocabulary entries of a partial sum: the same whatever the tile, so that a position's result is too
-constexpr int TILE_V = 256;         // vocabulary entries of a tile
+constexpr int TILE_V = 256;         // vocabulary entries that the gradient is cut by
 constexpr int PIECE = 8192;         // rows of a forward pass: 8 bytes per row and group of partial sums
 constexpr int UNITS = 256;          // workgroups of a kernel that walks tiles: one fills a compute unit
-constexpr float LOG2E = 1.4426950408889634f;
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
-struct Row { float inv_t, lse, scale; int32_t target; };   // scale = g inv_t; padding: all 0, target -1
+// Logits are held in powers of two: z log2(e).  factor = inv_t log2(e), lse2 = lse log2(e), scale = g inv_t; padding: all 0, target -1
+struct Row { float factor, lse2, scale; int32_t target; };
 
 // The workgroup numbers the positions with a target in order: each(position, has, number) for every position; returns how many there are.
 template <int THREADS, typename Each>
@@ -114,21 +115,22 @@ __global__ __launch_bounds__(256) void loss_gather_kernel(Head q, Positions at, 
   if (blockIdx.y == 0 && threadIdx.x < 32) {
     Row i{0.f, 0.f, 0.f, -1};
     if (t >= 0) {
-      i.inv_t = q.inv_t ? q.inv_t[t] : 1.f;
-      if (q.g) { i.lse = q.lse[t]; i.scale = q.g[t] * i.inv_t; }
+      const float inv_t = q.inv_t ? q.inv_t[t] : 1.f;
+      i.factor = inv_t >= 0.f ? inv_t * LOG2E : NAN;   // (the largest product has the largest logit)
+      if (q.g) { i.lse2 = q.lse[t] * LOG2E; i.scale = q.g[t] * inv_t; }
       i.target = q.target[t];
     }
     info[r] = i;
   }
 }
 
-// Logit tiles: 256 vocabulary entries from v_begin on x BN rows.  XCD i takes the i-th eighth of them; bands of 2048 rows, in a band vocabulary tile by
+// Logit tiles: BM vocabulary entries x BN rows.  XCD i takes the i-th eighth of them; bands of 2048 rows, in a band vocabulary tile by
 // vocabulary tile, so that an XCD's units share few operands at a time.
-template <int BN>
+template <int BM, int BN>
 struct LogitTiles {
   int nm, nv, at, end;
   __device__ __forceinline__ void init(int count, int n_v) {
-    nm = (count + BN - 1) / BN; nv = (n_v + TILE_V - 1) / TILE_V;
+    nm = (count + BN - 1) / BN; nv = (n_v + BM - 1) / BM;
     const int tiles = nm * nv, xcd = blockIdx.x & 7;
     at = xcd * (tiles >> 3) + min(xcd, tiles & 7);
     end = at + (tiles >> 3) + (xcd < (tiles & 7) ? 1 : 0);
@@ -145,8 +147,8 @@ struct LogitTiles {
 template <typename T>
 __device__ __forceinline__ Item logit_item(const Head &q, const bf16_t *op, int n_pad, int v_begin, int mt, int vt) {
   Item i;
-  i.row0 = mt * T::BN; i.col0 = v_begin + vt * TILE_V; i.kind = 0;
-  i.x = q.w + i.col0 * q.ldw; i.ldx = q.ldw; i.x_rows = min(q.vocab - i.col0, TILE_V);
+  i.row0 = mt * T::BN; i.col0 = v_begin + vt * T::BM; i.kind = 0;
+  i.x = q.w + i.col0 * q.ldw; i.ldx = q.ldw; i.x_rows = __builtin_amdgcn_readfirstlane(max(0, min(q.vocab - i.col0, T::BM)));   // (a vector instruction may have made it: the loads want it in a scalar register)
   i.w = op; i.w_n = n_pad; i.w_planes = i.ksteps = q.d / BK; i.w_row = i.row0;
   return i;
 }
@@ -160,7 +162,7 @@ __global__ __launch_bounds__(256) void loss_forward_kernel(Head q, const bf16_t 
   __shared__ __attribute__((aligned(1024))) bf16_t xs[T::LDS];
   const int count = min(*q.count - first, n_pad);
   if (count <= 0) return;
-  LogitTiles<T::BN> tiles;
+  LogitTiles<T::BM, T::BN> tiles;
   tiles.init(count, q.vocab);
   if (tiles.at >= tiles.end) return;
   T t;
@@ -185,7 +187,7 @@ __global__ __launch_bounds__(256) void loss_forward_kernel(Head q, const bf16_t 
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) z[h][i] = t.result(a + h, b, i) * row.inv_t;
+          for (int i = 0; i < 16; ++i) z[h][i] = t.result(a + h, b, i);
         if (v + GROUP > q.vocab) {   // (uniform: the last tile's entries beyond the vocabulary)
 #pragma unroll
           for (int h = 0; h < 2; ++h)
@@ -199,19 +201,20 @@ __global__ __launch_bounds__(256) void loss_forward_kernel(Head q, const bf16_t 
           for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-              if (y - t.half * 4 == h * 32 + (i >> 2) * 8 + (i & 3) && r < count) zt[r] = z[h][i];
+              if (y - t.half * 4 == h * 32 + (i >> 2) * 8 + (i & 3) && r < count) zt[r] = z[h][i] * row.factor;
         }
         float m = z[0][0];
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
           for (int i = 0; i < 16; ++i) m = fmaxf(m, z[h][i]);
-        m = with_xor32(m, OpMax{});
+        // (the rounding of m, which every difference shares, is in the sum too: m + log2 s is exact about it)
+        m = with_xor32(m, OpMax{}) * row.factor;
         float s = 0.f;
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) s += __builtin_amdgcn_exp2f((z[h][i] - m) * LOG2E);
+          for (int i = 0; i < 16; ++i) s += __builtin_amdgcn_exp2f(fmaf(z[h][i], row.factor, -m));
         s = with_xor32(s, OpSum{});
         if (t.half == 0 && r < count && v < q.vocab) parts[(int64_t)(v / GROUP) * n_pad + r] = make_float2(m, s);
 #ifdef __HIP_DEVICE_COMPILE__
@@ -234,7 +237,7 @@ __global__ __launch_bounds__(1024) void loss_merge_kernel(const float2 *__restri
   auto join = [](float &m, float &s, float2 p) {
     const float top = p.x > m || p.x != p.x ? p.x : m;
     if (top == -INFINITY) return;
-    s = s * __expf(m - top) + p.y * __expf(p.x - top);
+    s = s * __builtin_amdgcn_exp2f(m - top) + p.y * __builtin_amdgcn_exp2f(p.x - top);
     m = top;
   };
   const float2 none = make_float2(-INFINITY, 0.f);
@@ -257,10 +260,10 @@ __global__ __launch_bounds__(1024) void loss_merge_kernel(const float2 *__restri
   __syncthreads();
   if (at || r >= n) return;
   for (int i = 1; i < 8; ++i) join(m, s, joined[i][r16]);
-  const float l = m + logf(s);
+  const float l = log2f(s);
   const int t = rows[first + r];
-  lse[t] = l;
-  logprob[t] = zt[r] - l;
+  lse[t] = (m + l) * LN2;
+  logprob[t] = ((zt[r] - m) - l) * LN2;   // (a certain token's logit is m, to the last bit)
 }
 
 // a 32 x 32 block of results (a lane: one column, rows (i / 4) * 8 + half * 4 + i % 4) as two fragments of eight consecutive rows: 16 f + 8 half on
@@ -314,8 +317,8 @@ __global__ __launch_bounds__(256) void loss_grad_logits_kernel(Head q, const bf1
   const int64_t begin = (int64_t)index * cut.piece * TILE_V;
   if (begin >= q.vocab) return;
   const int v_begin = (int)begin, width = cut.piece * TILE_V, n_rows = (count + T::BN - 1) / T::BN * T::BN;
-  LogitTiles<T::BN> tiles;
-  tiles.init(count, min(width, q.vocab - v_begin));
+  LogitTiles<T::BM, T::BN> tiles;
+  tiles.init(count, min(width, (q.vocab - v_begin + TILE_V - 1) / TILE_V * TILE_V));   // (zeros behind the vocabulary, to a whole tile of the products)
   if (tiles.at >= tiles.end) return;
   T t;
   t.init_at(xs);
@@ -337,7 +340,7 @@ __global__ __launch_bounds__(256) void loss_grad_logits_kernel(Head q, const bf1
         const int v = v0 + a * 32, v32 = (v - v_begin) >> 5, y = row.target - v;
         float G[16];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) G[i] = -row.scale * __builtin_amdgcn_exp2f((t.result(a, b, i) * row.inv_t - row.lse) * LOG2E);
+        for (int i = 0; i < 16; ++i) G[i] = -row.scale * __builtin_amdgcn_exp2f(fmaf(t.result(a, b, i), row.factor, -row.lse2));
         if (__ballot(y >= 0 && y < 32)) {
 #pragma unroll
           for (int i = 0; i < 16; ++i)
@@ -575,8 +578,9 @@ struct ForwardSpace {
   }
 };
 
-// Elements of a piece's G.  (7B shape, 4096 positions: @MOST@.)
-constexpr int64_t GRAD_MOST = (int64_t)96 << 20;
+// Elements of a piece's G.  More takes fewer launches whose last tiles leave units without work (7B shape, 3328
+// rows, 48 / 96 / 192 / 384 Mi: 9.79 / 8.71 / 8.49 / 8.40 ms), and memory.
+constexpr int64_t GRAD_MOST = (int64_t)192 << 20;
 constexpr int NUMBER_MOST = 1024;   // positions that the gather's workgroups number for themselves
 
 struct GradSpace {
@@ -614,14 +618,14 @@ int grad_pieces(int n_pad, int vocab, int d, int64_t ldw) {
   return most;
 }
 
-// calls f(rows of a tile, a kernel's shape as constants)
+// Calls f(a kernel's shape as constants, workgroups) for logits of up to n rows.  Few rows stream W: tiles of 128 entries, of which two are on a unit and
+// the last ones leave fewer units without work than 256 of them do (1.5B shape, 61 positions: @NARROW@).
 template <typename F>
-void with_shape(int n, bool narrow, F f) {
+void with_shape(int n, F f) {
   using std::integral_constant;
-  if (narrow && n <= 32) f(integral_constant<int, 4>{}, integral_constant<int, 1>{}, integral_constant<int, 2>{}, integral_constant<int, 1>{});
-  else if (n <= 64) f(integral_constant<int, 4>{}, integral_constant<int, 1>{}, integral_constant<int, 2>{}, integral_constant<int, 2>{});
-  else if (n <= 128) f(integral_constant<int, 2>{}, integral_constant<int, 2>{}, integral_constant<int, 4>{}, integral_constant<int, 2>{});
-  else f(integral_constant<int, 1>{}, integral_constant<int, 4>{}, integral_constant<int, 8>{}, integral_constant<int, 2>{});
+  if (n <= 64) f(integral_constant<int, 2>{}, integral_constant<int, 2>{}, integral_constant<int, 2>{}, integral_constant<int, 1>{}, 2 * UNITS);
+  else if (n <= 128) f(integral_constant<int, 2>{}, integral_constant<int, 2>{}, integral_constant<int, 2>{}, integral_constant<int, 2>{}, 2 * UNITS);
+  else f(integral_constant<int, 1>{}, integral_constant<int, 4>{}, integral_constant<int, 8>{}, integral_constant<int, 2>{}, UNITS);
 }
 
 }  // namespace
@@ -637,8 +641,8 @@ int launch_token_logprob(const TokenLoss &p, float *logprob, float *lse, hipStre
   for (int first = 0; first < p.n; first += PIECE) {
     auto gather = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(w.n_pad / 32, p.d / 64), dim3(256), 0, s, q, at, first, w.op, (bf16_t *)nullptr, w.info); };
     if (number) gather(loss_gather_kernel<true>); else gather(loss_gather_kernel<false>);
-    with_shape(std::min(p.n - first, PIECE), true, [&](auto WM, auto WN, auto AT, auto BT) {
-      auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(UNITS), dim3(256), 0, s, q, w.op, w.info, w.parts, w.zt, first, w.n_pad); };
+    with_shape(std::min(p.n - first, PIECE), [&](auto WM, auto WN, auto AT, auto BT, int grid) {
+      auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, s, q, w.op, w.info, w.parts, w.zt, first, w.n_pad); };
       constexpr bool once = WM.value > 1;   // (tiles of up to 128 rows: there is one of them)
       launch(loss_forward_kernel<WM.value, WN.value, AT.value, BT.value, once>);
     });
@@ -658,9 +662,9 @@ int launch_token_logprob_grad(const TokenLoss &p, const float *lse, const float 
   auto gather = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(w.n_pad / 32, p.d / 64), dim3(256), 0, s, q, at, 0, w.op, w.turned, w.info); };
   if (number) gather(loss_gather_kernel<true>); else gather(loss_gather_kernel<false>);
   const int pieces = grad_pieces(w.n_pad, p.vocab, p.d, p.ldw);
-  with_shape(p.n, false, [&](auto WM, auto WN, auto AT, auto BT) {
+  with_shape(p.n, [&](auto WM, auto WN, auto AT, auto BT, int grid) {
     for (int i = 0; i < pieces; ++i) {
-      hipLaunchKernelGGL((loss_grad_logits_kernel<WM.value, WN.value, AT.value, BT.value>), dim3(UNITS), dim3(256), 0, s, q, w.op, w.info, w.G, i, GRAD_MOST,
+      hipLaunchKernelGGL((loss_grad_logits_kernel<WM.value, WN.value, AT.value, BT.value>), dim3(grid), dim3(256), 0, s, q, w.op, w.info, w.G, i, GRAD_MOST,
                          w.n_pad, w.tickets);
       const GradParams gp{w.G, w.turned, dh ? w.dh32 : nullptr, dw, w.tickets, GRAD_MOST, i, w.n_pad, WN.value * BT.value * 32};
       hipLaunchKernelGGL(loss_grad_kernel, dim3(UNITS), dim3(256), 0, s, q, gp);
