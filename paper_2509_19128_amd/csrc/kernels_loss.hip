@@ -225,14 +225,15 @@ __global__ __launch_bounds__(256) void loss_forward_kernel(Head q, const bf16_t 
   });
 }
 
-// The groups of sixteen rows joined, by 64 threads per row: each takes every 64th group in order, then their results are joined, eight at a time, in
-// order.
+// The groups of JOIN_ROWS rows joined, by JOIN threads per row: each takes every JOINth group in order, then their results are joined, sixteen at a time and
+// the rest, in order.  (One number of threads for every call: a row's result is to be the same in all.)
+constexpr int JOIN_ROWS = 8, JOIN = 1024 / JOIN_ROWS;
 __global__ __launch_bounds__(1024) void loss_merge_kernel(const float2 *__restrict__ parts, const float *__restrict__ zt, const int32_t *__restrict__ rows,
                                                           const int32_t *__restrict__ count, float *__restrict__ logprob, float *__restrict__ lse, int groups, int first,
                                                           int n_pad) {
-  __shared__ float2 joined[64][16];
-  const int r16 = threadIdx.x & 15, at = threadIdx.x >> 4, r = blockIdx.x * 16 + r16, n = min(*count - first, n_pad);
-  if ((int)blockIdx.x * 16 >= n) return;
+  __shared__ float2 joined[JOIN][JOIN_ROWS];
+  const int row = threadIdx.x % JOIN_ROWS, at = threadIdx.x / JOIN_ROWS, r = blockIdx.x * JOIN_ROWS + row, n = min(*count - first, n_pad);
+  if ((int)blockIdx.x * JOIN_ROWS >= n) return;
   // (no entries: -inf, 0; NaN stays)
   auto join = [](float &m, float &s, float2 p) {
     const float top = p.x > m || p.x != p.x ? p.x : m;
@@ -242,24 +243,25 @@ __global__ __launch_bounds__(1024) void loss_merge_kernel(const float2 *__restri
   };
   const float2 none = make_float2(-INFINITY, 0.f);
   float m = -INFINITY, s = 0.f;
-  for (int g = at; g < groups; g += 64 * 8) {
-    float2 p[8];
+  for (int g = at; g < groups; g += JOIN * 4) {
+    float2 p[4];
 #pragma unroll
-    for (int u = 0; u < 8; ++u) p[u] = g + u * 64 < groups && r < n ? parts[(int64_t)(g + u * 64) * n_pad + r] : none;
+    for (int u = 0; u < 4; ++u) p[u] = g + u * JOIN < groups && r < n ? parts[(int64_t)(g + u * JOIN) * n_pad + r] : none;
 #pragma unroll
-    for (int u = 0; u < 8; ++u) join(m, s, p[u]);
+    for (int u = 0; u < 4; ++u) join(m, s, p[u]);
   }
-  joined[at][r16] = make_float2(m, s);
-  __syncthreads();
-  if (at < 8) {
-    m = -INFINITY; s = 0.f;
-    for (int i = 0; i < 8; ++i) join(m, s, joined[at * 8 + i][r16]);
+  joined[at][row] = make_float2(m, s);
+#pragma unroll
+  for (int left = JOIN / 16, many = 16; left > 0; many = left, left = left > 1 ? 1 : 0) {
+    __syncthreads();
+    if (at < left) {
+      m = -INFINITY; s = 0.f;
+      for (int i = 0; i < many; ++i) join(m, s, joined[at * many + i][row]);
+    }
+    __syncthreads();
+    if (at < left) joined[at][row] = make_float2(m, s);
   }
-  __syncthreads();
-  if (at < 8) joined[at][r16] = make_float2(m, s);
-  __syncthreads();
   if (at || r >= n) return;
-  for (int i = 1; i < 8; ++i) join(m, s, joined[i][r16]);
   const float l = log2f(s);
   const int t = rows[first + r];
   lse[t] = (m + l) * LN2;
@@ -372,22 +374,27 @@ struct GradParams {
   int index, n_pad, tile_rows;              // the piece; rows of `turned`; rows of a tile of the kernel that made G
 };
 
-// Tiles that the units take by tickets, from their own XCD's eighth and, when that is done, from the others'.  One thread draws; the others read what it
-// leaves in LDS.  A ticket is asked for as a tile begins and looked at when the tile is nearly done.
+// Tiles that the units take by tickets, from their own XCD's eighth and, when that is done, from the others'.  The first ones are dealt without a ticket,
+// one to each unit whose hands `before` tiles of another kind leave empty: of tiles as long as those of dh no unit is to take a second one while
+// another has none.  One thread draws; the others read what it leaves in LDS.  A ticket is asked for as a tile begins and looked at when the
+// tile is nearly done.
 struct Lottery {
   int32_t *tickets;   // eight, 128 bytes apart
-  int n, dealt, asked, from;
-  bool own;           // tickets of this XCD's eighth may be left
-  // dealt: so many of each eighth go one to each unit, without a ticket (tiles of which a unit is to take no second one while another has none)
-  __device__ __forceinline__ Lottery(int32_t *t, int n_, int dealt_) : tickets(t), n(n_), dealt(dealt_), asked(0), from(0), own(true) {}
-  __device__ __forceinline__ int first(int x) const { return x * (n >> 3) + min(x, n & 7); }
-  __device__ __forceinline__ int size(int x) const { return first(x + 1) - first(x); }
+  int n, before, asked, from;
+  bool own, any;      // tickets of this XCD's eighth, of any eighth may be left
+  __device__ __forceinline__ Lottery(int32_t *t, int n_, int before_) : tickets(t), n(n_), before(before_), asked(0), from(0), own(true), any(false) {
+    for (int x = 0; x < 8; ++x) any |= size(x) > dealt(x);
+  }
+  static __device__ __forceinline__ int first(int n, int x) { return x * (n >> 3) + min(x, n & 7); }
+  __device__ __forceinline__ int size(int x) const { return first(n, x + 1) - first(n, x); }
+  __device__ __forceinline__ int busy(int x) const { return first(before, x + 1) - first(before, x); }   // units of an XCD that hold another tile
+  __device__ __forceinline__ int dealt(int x) const { return max(0, UNITS / 8 - busy(x)); }
   __device__ __forceinline__ int draw(int x) const {
-    return size(x) <= dealt ? size(x) : dealt + __hip_atomic_fetch_add(&tickets[x * 32], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return size(x) <= dealt(x) ? size(x) : dealt(x) + __hip_atomic_fetch_add(&tickets[x * 32], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
   // a tile of another eighth, or -1: an eighth that looks unfinished is asked, and one that was finished meanwhile looks so the next time
   __device__ __forceinline__ int steal() const {
-    for (;;) {
+    while (any) {
       int seen[8];
 #pragma unroll
       for (int k = 0; k < 8; ++k) seen[k] = __hip_atomic_load(&tickets[((blockIdx.x + k) & 7) * 32], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -395,21 +402,23 @@ struct Lottery {
 #pragma unroll
       for (int k = 7; k >= 0; --k) {
         const int y = (blockIdx.x + k) & 7;
-        if (dealt + seen[k] < size(y)) x = y;
+        if (dealt(y) + seen[k] < size(y)) x = y;
       }
-      if (x < 0) return -1;
+      if (x < 0) break;
       const int i = draw(x);
-      if (i < size(x)) return first(x) + i;
+      if (i < size(x)) return first(n, x) + i;
     }
+    return -1;
   }
   // the first two tiles
   template <typename Place>
   __device__ __forceinline__ void begin(Place place) {
-    const int x = blockIdx.x & 7;
-    from = first(x);
+    const int x = blockIdx.x & 7, turn = (int)(blockIdx.x >> 3) - busy(x);
+    from = first(n, x);
     int a = -1;
-    if ((int)(blockIdx.x >> 3) < min(dealt, size(x))) a = from + (blockIdx.x >> 3);
-    else if (dealt == 0) {
+    if (turn >= 0) {
+      if (turn < size(x)) a = from + turn;
+    } else {
       ask();
       a = told();
     }
@@ -444,8 +453,8 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(Head q, GradParams g) {
   const int64_t g_plane = (int64_t)g_rows * 64;
   const int k_all = nv * (TILE_V / BK), k_slice = cut.slice * (TILE_V / BK);
   // the walk over one kind of tile
-  auto tiles = [&](auto &t, int n, int dealt, int32_t *tickets, auto item, auto done) {
-    Lottery lots(tickets, n, dealt);
+  auto tiles = [&](auto &t, int n, int before, int32_t *tickets, auto item, auto done) {
+    Lottery lots(tickets, n, before);
     const bool draws = threadIdx.x == 0;
     if (draws) lots.begin([&](int i, int v) { drawn[i] = v; });
     __syncthreads();
@@ -464,9 +473,10 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(Head q, GradParams g) {
     }, done);
     __syncthreads();
   };
-  if (g.dh32 && nm > 0) {
+  const int n_dh = g.dh32 ? (k_all + k_slice - 1) / k_slice * nm * nd : 0;
+  if (n_dh > 0) {
     TH t;
-    tiles(t, (k_all + k_slice - 1) / k_slice * nm * nd, UNITS / 8, g.tickets, [&](int i) {
+    tiles(t, n_dh, 0, g.tickets, [&](int i) {
       Item c;
       const int dt = i % nd, rest = i / nd, mt = rest % nm, k0 = rest / nm * k_slice, v = v_begin + k0 * BK;
       c.kind = rest / nm; c.row0 = mt * 256; c.col0 = dt * 256; c.ksteps = min(k_slice, k_all - k0);
@@ -498,7 +508,7 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(Head q, GradParams g) {
   if (g.dw) {
     // G's rows behind its last tile do not exist: the last k-steps take other entries' rows in their place, against zeros of h^T
     TW t;
-    tiles(t, nv * nd, 0, g.tickets + 8 * 32, [&](int i) {
+    tiles(t, nv * nd, n_dh, g.tickets + 8 * 32, [&](int i) {
       Item c;
       const int dt = i % nd, vt = i / nd;
       c.kind = 0; c.row0 = vt * TILE_V; c.col0 = dt * 256; c.ksteps = max(4, (g_rows / BK + 3) / 4 * 4);
@@ -539,6 +549,7 @@ __global__ __launch_bounds__(256) void loss_round_kernel(const float *__restrict
   const int slices = cut.slices, n_pad = cut.nm * 256;
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
   if (r >= 0)
+#pragma unroll 8
     for (int s = 0; s < slices; ++s) v += *(const f32x4 *)(dh32 + ((int64_t)s * n_pad + r) * d + k);
   bf16x4 o;
 #pragma unroll
@@ -646,7 +657,7 @@ int launch_token_logprob(const TokenLoss &p, float *logprob, float *lse, hipStre
       constexpr bool once = WM.value > 1;   // (tiles of up to 128 rows: there is one of them)
       launch(loss_forward_kernel<WM.value, WN.value, AT.value, BT.value, once>);
     });
-    hipLaunchKernelGGL(loss_merge_kernel, dim3(w.n_pad / 16), dim3(1024), 0, s, w.parts, w.zt, w.rows, w.count, logprob, lse, w.groups, first, w.n_pad);
+    hipLaunchKernelGGL(loss_merge_kernel, dim3((std::min(p.n - first, w.n_pad) + JOIN_ROWS - 1) / JOIN_ROWS), dim3(1024), 0, s, w.parts, w.zt, w.rows, w.count, logprob, lse, w.groups, first, w.n_pad);
   }
   return done();
 }
