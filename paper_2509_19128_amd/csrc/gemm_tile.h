@@ -48,7 +48,8 @@ constexpr int W_CACHE = WM == 1 && COLD ? 2 : 0;
 // k rows of a read lie in different banks; TILE_ROWS_T, W first again, with x an operand-ordered image taken across: the image's k are rows of x, its rows
 // are k.  LDS holds, for each chunk of eight rows of x, 64 k of 16 bytes, number m at slot m ^ 4 (chunk & 3), read by transposing too.
 enum { TILE_ROWS, TILE_INT8, TILE_COLS, TILE_COLS_T, TILE_ROWS_T };
-template <int WM, int WN, int AT, int BT, bool COLD, int KIND = TILE_ROWS>
+// W_ROWS (TILE_COLS): W's rows too as they lie, wherever each is: few, and found again in the caches.
+template <int WM, int WN, int AT, int BT, bool COLD, int KIND = TILE_ROWS, bool W_ROWS = false>
 struct Tile {
   static constexpr int BM = WM * AT * 32, BN = WN * BT * 32;
   static constexpr int XI = BM / 32, XH = (XI + 1) / 2, WI = BT * 4;   // loads of a wavefront per k-step: x (half of them XH), W
@@ -73,6 +74,7 @@ struct Tile {
   __amdgpu_buffer_rsrc_t rw, rx;   // one resource per operand; what is uniform across a wavefront is in scalar registers
   uint32_t w_plane;
   int wave, wm, wn, l, lrow, half, a_off[4];
+  int w_lane[BT];                  // W_ROWS: byte offset of the lane's row and half
   int x_step, x_load;              // bytes from a k-step of x to the next, and from a wavefront's load of 64 chunks to the next (other kinds than TILE_ROWS)
   bf16_t *xs;
   typedef std::conditional_t<KIND == TILE_INT8, i32x16, f32x16> Acc;
@@ -122,13 +124,16 @@ struct Tile {
       }
     }
   }
+  // W_ROWS: the rows within `bytes` from W on; row b of the lane at element `at` (negative: none, zeros)
+  __device__ __forceinline__ void rows_w(const bf16_t *W, int bytes) { rw = __builtin_amdgcn_make_buffer_rsrc((void *)W, 0, bytes, 0x00020000); }
+  __device__ __forceinline__ void row_w(int b, int at) { w_lane[b] = at < 0 ? 0x7fff0000 : at * 2 + half * 64; }
   // x: rows (TILE_COLS_T: k) ldx elements apart from X on, of which `rows` exist (further ones read as 0); TILE_ROWS_T: an image of ldx rows, from the plane at
   // X on, of which `rows` planes of 64 exist;
   // w: operand-ordered, `n` of its rows per plane and `planes` k-steps from W on (further ones read as 0), the tile's from w_row on.
   __device__ __forceinline__ Part part_at(const bf16_t *X, int64_t ldx, int rows, const bf16_t *W, int n, int planes, int w_row) {
     Part p;
     w_plane = (uint32_t)(n >> 5) * 4096u;
-    rw = __builtin_amdgcn_make_buffer_rsrc((void *)W, 0, (int)((uint32_t)planes * w_plane), 0x00020000);
+    if (!W_ROWS) rw = __builtin_amdgcn_make_buffer_rsrc((void *)W, 0, (int)((uint32_t)planes * w_plane), 0x00020000);
     const int64_t x_bytes = (int64_t)rows * ldx * (KIND == TILE_ROWS_T ? 128 : 2);
     rx = __builtin_amdgcn_make_buffer_rsrc((void *)X, 0, (int)min(x_bytes, (int64_t)0x7fffffff), 0x00020000);
     constexpr int PER = KIND == TILE_COLS_T ? BM / 8 : BK / 8, ROWS = 64 / PER;   // chunks of a row (of 64 k or of BM columns), rows of a load
@@ -174,7 +179,8 @@ struct Tile {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
       wf[st][b][j] = __builtin_bit_cast(
-          bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rw, l * 16 + j * 1024, (int)(p.w_blk[b] + (uint32_t)ks * w_plane), W_CACHE<WM, COLD>));
+          bf16x8, W_ROWS ? __builtin_amdgcn_raw_buffer_load_b128(rw, w_lane[b] + j * 16, ks * (BK * 2), 0)
+                         : __builtin_amdgcn_raw_buffer_load_b128(rw, l * 16 + j * 1024, (int)(p.w_blk[b] + (uint32_t)ks * w_plane), W_CACHE<WM, COLD>));
   }
   __device__ __forceinline__ void load(const Part &p, int st, int ks) {
     load_x(p, st, ks, 0, XI);

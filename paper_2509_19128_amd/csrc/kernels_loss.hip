@@ -27,6 +27,7 @@ constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 // Logits are held in powers of two: z log2(e).  factor = inv_t log2(e), lse2 = lse log2(e), scale = g inv_t; padding: all 0, target -1
 struct Row { float factor, lse2, scale; int32_t target; };
+__device__ inline float logit_factor(float inv_t) { return inv_t >= 0.f ? inv_t * LOG2E : NAN; }   // (not negative: the largest product has the largest logit)
 
 // The workgroup numbers the positions with a target in order: each(position, has, number) for every position; returns how many there are.
 template <int THREADS, typename Each>
@@ -53,12 +54,39 @@ __device__ __forceinline__ int number_positions(const int32_t *__restrict__ targ
   return base;
 }
 
+// How many positions have a target, which the device finds out, and how the gradient is cut for so many rows: vocabulary tiles of a piece, tiles of a slice
+// of dh along a piece, and slices.  A piece's G takes at most `most` tiles of 256 x 256 (or one vocabulary tile's); its tiles are whole rounds of the
+// units where there are that many.  Slices of dh: until there are as many tiles as units (each is a sum of its own that is read and written per piece).
+struct Cut {
+  int count, nm, piece, slice, slices;
+  static __host__ __device__ int slices_most(int nm, int d) {
+    const int tiles = nm * (d / 256), s = tiles > 0 ? UNITS / tiles : 1;
+    return s < 1 ? 1 : s > 16 ? 16 : s;
+  }
+  static __host__ __device__ Cut of(int count, int vocab, int d, int64_t ldw, int most) {
+    Cut c;
+    c.count = count;
+    c.nm = (count + 255) / 256;
+    const int tiles = (vocab + TILE_V - 1) / TILE_V, fit = most / (c.nm > 0 ? c.nm : 1), far = (1 << 22) / (int)ldw;   // (W's rows of a piece lie behind one 32-bit offset)
+    int p = fit < far ? fit : far;
+    if (p < 1) p = 1;
+    if (c.nm > 0 && c.nm * p >= UNITS) p = c.nm * p / UNITS * UNITS / c.nm;
+    c.piece = p < tiles ? p : tiles;
+    const int s = slices_most(c.nm, d);
+    c.slice = (c.piece + s - 1) / s;
+    c.slices = (c.piece + c.slice - 1) / c.slice;
+    return c;
+  }
+};
+
 // What is known of the positions: how many have a target, which, and the way back (place, may be null); zeros for the others (logprob and lse may be null).
 struct Positions {
   const int32_t *target;
-  int32_t *count, *rows, *place;
+  Cut *cut;
+  int32_t *rows, *place;
   float *logprob, *lse;
-  int n, vocab;
+  int n, vocab, d, most;
+  int64_t ldw;
   __device__ __forceinline__ void note(int t, bool has, int number) const {
     if (has) rows[number] = t;
     if (place) place[t] = has ? number : -1;
@@ -67,7 +95,7 @@ struct Positions {
 };
 __global__ __launch_bounds__(1024) void loss_rows_kernel(Positions q) {
   const int count = number_positions<1024>(q.target, q.n, q.vocab, [&](int t, bool has, int number) { q.note(t, has, number); });
-  if (threadIdx.x == 0) *q.count = count;
+  if (threadIdx.x == 0) *q.cut = Cut::of(count, q.vocab, q.d, q.ldw, q.most);
 }
 
 struct Head {
@@ -75,7 +103,8 @@ struct Head {
   int64_t ldh, ldw;
   const int32_t *target;
   const float *inv_t, *lse, *g;   // inv_t, or lse and g, may be null
-  const int32_t *rows, *count;
+  const int32_t *rows;
+  const Cut *cut;
   int vocab, d;
 };
 
@@ -94,9 +123,9 @@ __global__ __launch_bounds__(256) void loss_gather_kernel(Head q, Positions at, 
       if (has && (uint32_t)(number - r0) < 32u) mine[number - r0] = u;
       if (note) at.note(u, has, number);
     });
-    if (note && threadIdx.x == 0) *at.count = count;
+    if (note && threadIdx.x == 0) *at.cut = Cut::of(count, at.vocab, at.d, at.ldw, at.most);
     t = mine[threadIdx.x & 31];   // (number_positions ends behind a barrier; n >= 1)
-  } else if (r < *q.count - first) {
+  } else if (r < q.cut->count - first) {
     t = q.rows[first + r];
   }
   const uint4 v = t >= 0 ? *(const uint4 *)(q.h + t * q.ldh + k) : make_uint4(0, 0, 0, 0);
@@ -116,7 +145,7 @@ __global__ __launch_bounds__(256) void loss_gather_kernel(Head q, Positions at, 
     Row i{0.f, 0.f, 0.f, -1};
     if (t >= 0) {
       const float inv_t = q.inv_t ? q.inv_t[t] : 1.f;
-      i.factor = inv_t >= 0.f ? inv_t * LOG2E : NAN;   // (the largest product has the largest logit)
+      i.factor = logit_factor(inv_t);
       if (q.g) { i.lse2 = q.lse[t] * LOG2E; i.scale = q.g[t] * inv_t; }
       i.target = q.target[t];
     }
@@ -154,19 +183,52 @@ __device__ __forceinline__ Item logit_item(const Head &q, const bf16_t *op, int 
 }
 
 // (max, sum of exponentials) of each row and group of vocabulary entries; the logit of the target from the tile that has it
-// COLD: one tile of rows, so that W is read once.  1.5B shape, 61 positions: @COLD@.
-template <int WM, int WN, int AT, int BT, bool COLD>
-__global__ __launch_bounds__(256) void loss_forward_kernel(Head q, const bf16_t *__restrict__ op, const Row *__restrict__ info, float2 *__restrict__ parts, float *__restrict__ zt,
-                                                           int first, int n_pad) {
-  typedef Tile<WM, WN, AT, BT, COLD, TILE_COLS> T;
-  __shared__ __attribute__((aligned(1024))) bf16_t xs[T::LDS];
-  const int count = min(*q.count - first, n_pad);
+// COLD: one tile of rows, so that W is read once.
+// DIRECT: few positions, which every workgroup numbers for itself and whose rows it takes as they lie, each lane from another: no launch ahead, and lanes
+// without a row load nothing.  us, with the gather / so: tiny shape 14.6 / 12.1, 1.5B 4 positions 89.9 / 79.7, 32 90.3 / 87.5, 48 90.7 / 95.7; 152064 x
+// 5120 4 positions 273 / 242 (6.4 TB/s), 32 273 / 273.
+constexpr int DIRECT_MOST = 32;
+template <int WM, int WN, int AT, int BT, bool COLD, bool DIRECT>
+__global__ __launch_bounds__(256) void loss_forward_kernel(Head q, Positions at, const bf16_t *__restrict__ op, const Row *__restrict__ info, float2 *__restrict__ parts,
+                                                           float *__restrict__ zt, int first, int n_pad) {
+  typedef Tile<WM, WN, AT, BT, COLD, TILE_COLS, DIRECT> T;
+  __shared__ __attribute__((aligned(1024))) bf16_t xs[T::LDS + (DIRECT ? 128 : 0)];
+  int count;
+  T t;
+  t.init_at(xs);
+  float factor[BT];
+  int target[BT];
+  if constexpr (DIRECT) {
+    typedef __attribute__((address_space(3))) int32_t lds_int;
+    lds_int *mine = (lds_int *)(xs + T::LDS);
+    const bool in = t.l < at.n, has = in && (uint32_t)at.target[in ? t.l : 0] < (uint32_t)q.vocab;
+    const uint64_t mask = __ballot(has);
+    const int number = __popcll(mask & (((uint64_t)1 << t.l) - 1));
+    count = __popcll(mask);
+    if (t.wave == 0) {
+      if (has) mine[number] = t.l;
+      if (blockIdx.x == 0) {
+        if (in) at.note(t.l, has, number);
+        if (t.l == 0) at.cut->count = count;
+      }
+    }
+    __syncthreads();
+    t.rows_w(q.h, (int)(((at.n - 1) * q.ldh + q.d) * 2));
+#pragma unroll
+    for (int b = 0; b < BT; ++b) {
+      const int r = (t.wn * BT + b) * 32 + t.lrow, row = r < count ? mine[r] : -1;
+      t.row_w(b, row < 0 ? -1 : (int)(row * q.ldh));
+      const float inv_t = row >= 0 && q.inv_t ? q.inv_t[row] : 1.f;
+      factor[b] = logit_factor(inv_t);
+      target[b] = row >= 0 ? q.target[row] : -1;
+    }
+  } else {
+    count = min(q.cut->count - first, n_pad);
+  }
   if (count <= 0) return;
   LogitTiles<T::BM, T::BN> tiles;
   tiles.init(count, q.vocab);
   if (tiles.at >= tiles.end) return;
-  T t;
-  t.init_at(xs);
   walk(t, [] {}, [] {}, [&](Item &d) {
     if (tiles.at >= tiles.end) return false;
     int mt, vt;
@@ -179,7 +241,9 @@ __global__ __launch_bounds__(256) void loss_forward_kernel(Head q, const bf16_t 
 #pragma unroll
     for (int b = 0; b < BT; ++b) {
       const int r = c.row0 + (t.wn * BT + b) * 32 + t.lrow;
-      const Row row = info[r];
+      Row row;
+      if constexpr (DIRECT) { row.factor = factor[b]; row.target = target[b]; }
+      else row = info[r];
 #pragma unroll
       for (int a = 0; a < AT; a += 2) {
         const int v = v0 + a * 32;   // a group
@@ -229,10 +293,10 @@ __global__ __launch_bounds__(256) void loss_forward_kernel(Head q, const bf16_t 
 // the rest, in order.  (One number of threads for every call: a row's result is to be the same in all.)
 constexpr int JOIN_ROWS = 8, JOIN = 1024 / JOIN_ROWS;
 __global__ __launch_bounds__(1024) void loss_merge_kernel(const float2 *__restrict__ parts, const float *__restrict__ zt, const int32_t *__restrict__ rows,
-                                                          const int32_t *__restrict__ count, float *__restrict__ logprob, float *__restrict__ lse, int groups, int first,
+                                                          const Cut *__restrict__ cut, float *__restrict__ logprob, float *__restrict__ lse, int groups, int first,
                                                           int n_pad) {
   __shared__ float2 joined[JOIN][JOIN_ROWS];
-  const int row = threadIdx.x % JOIN_ROWS, at = threadIdx.x / JOIN_ROWS, r = blockIdx.x * JOIN_ROWS + row, n = min(*count - first, n_pad);
+  const int row = threadIdx.x % JOIN_ROWS, at = threadIdx.x / JOIN_ROWS, r = blockIdx.x * JOIN_ROWS + row, n = min(cut->count - first, n_pad);
   if ((int)blockIdx.x * JOIN_ROWS >= n) return;
   // (no entries: -inf, 0; NaN stays)
   auto join = [](float &m, float &s, float2 p) {
@@ -286,36 +350,15 @@ __device__ __forceinline__ int64_t fragment_place(int row, int k32, int n, int f
   return ((((int64_t)(k32 >> 1) * (n >> 5) + row) * 4 + 2 * f + half) * 64 + (k32 & 1) * 32 + lrow) * 16;
 }
 
-// How the gradient is cut, from the number of rows, which the device knows: vocabulary tiles of a piece, tiles of a slice of dh along a piece, and slices.
-// A piece's G takes at most `most` elements (or one vocabulary tile's); its tiles of 256 rows are whole rounds of the units where there
-// are that many.  Slices of dh: until there are as many tiles as units (each is a sum of its own that is read and written per piece).
-struct GradCut {
-  int nm, piece, slice, slices, slices_most;   // (slices_most: of any piece of this many rows)
-  __host__ __device__ GradCut(int count, int v_tiles, int d, int64_t ldw, int64_t most) {
-    nm = (count + 255) / 256;
-    const int64_t fit = most / 65536 / (nm > 0 ? nm : 1), far = ((int64_t)1 << 30) / ldw / 256;   // (W's rows of a piece lie behind one 32-bit offset)
-    int64_t p = fit < far ? fit : far;
-    if (p < 1) p = 1;
-    if (nm > 0 && nm * p >= UNITS) p = nm * p / UNITS * UNITS / nm;
-    piece = p < v_tiles ? (int)p : v_tiles;
-    const int tiles = nm * (d / 256);
-    int s = tiles > 0 ? UNITS / tiles : 1;
-    s = s < 1 ? 1 : s > 16 ? 16 : s;
-    slices_most = s;
-    slice = (piece + s - 1) / s;
-    slices = (piece + slice - 1) / slice;
-  }
-};
-
 // G of a piece of the vocabulary, in operand order (a row's entries are its k; rows to whole tiles).  Clears the tickets of the kernel behind.
 template <int WM, int WN, int AT, int BT>
 __global__ __launch_bounds__(256) void loss_grad_logits_kernel(Head q, const bf16_t *__restrict__ op, const Row *__restrict__ info, bf16_t *__restrict__ G_out,
-                                                               int index, int64_t most, int n_pad, int32_t *__restrict__ tickets) {
+                                                               int index, int n_pad, int32_t *__restrict__ tickets) {
   typedef Tile<WM, WN, AT, BT, false, TILE_COLS> T;
   __shared__ __attribute__((aligned(1024))) bf16_t xs[T::LDS];
   if (blockIdx.x == 0 && threadIdx.x < 16) tickets[threadIdx.x * 32] = 0;
-  const int count = *q.count;
-  const GradCut cut(count, (q.vocab + TILE_V - 1) / TILE_V, q.d, q.ldw, most);
+  const Cut cut = *q.cut;
+  const int count = cut.count;
   const int64_t begin = (int64_t)index * cut.piece * TILE_V;
   if (begin >= q.vocab) return;
   const int v_begin = (int)begin, width = cut.piece * TILE_V, n_rows = (count + T::BN - 1) / T::BN * T::BN;
@@ -370,7 +413,6 @@ struct GradParams {
   float *dh32;                              // [slices][rows, to a multiple of 256][d], or null: no dh
   bf16_t *dw;                               // or null
   int32_t *tickets;                         // sixteen, 128 bytes apart, zero: eight of each kind of tile
-  int64_t most;
   int index, n_pad, tile_rows;              // the piece; rows of `turned`; rows of a tile of the kernel that made G
 };
 
@@ -444,8 +486,8 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(Head q, GradParams g) {
   __shared__ __attribute__((aligned(1024))) bf16_t xs[TH::LDS + 4];
   typedef __attribute__((address_space(3))) volatile int32_t lds_int;
   lds_int *drawn = (lds_int *)(xs + TH::LDS);
-  const int count = *q.count, nd = q.d / 256;
-  const GradCut cut(count, (q.vocab + TILE_V - 1) / TILE_V, q.d, q.ldw, g.most);
+  const Cut cut = *q.cut;
+  const int count = cut.count, nd = q.d / 256;
   const int64_t begin = (int64_t)g.index * cut.piece * TILE_V;
   if (begin >= q.vocab) return;
   const int v_begin = (int)begin, nm = cut.nm, nv = min(cut.piece, (q.vocab - v_begin + TILE_V - 1) / TILE_V), n_rows = nm * 256;
@@ -516,10 +558,11 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(Head q, GradParams g) {
       c.w = g.turned; c.w_n = q.d; c.w_planes = g_rows / BK; c.w_row = c.col0;
       return c;
     }, [&](const Item &c) {
+      // (the stores that fill a line behind each other: 1.5B shape, 61 / 777 positions, 393 / 669 -> 357 / 647 us)
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
+      for (int a = 0; a < 8; ++a) {
 #pragma unroll
-        for (int a = 0; a < 8; ++a) {
+        for (int b = 0; b < 2; ++b) {
           const int v = v_begin + c.row0 + a * 32 + t.lrow;
           float s[16];
 #pragma unroll
@@ -542,11 +585,10 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(Head q, GradParams g) {
 
 // dh of every position: the slices of its row added up in order and rounded, or zeros
 __global__ __launch_bounds__(256) void loss_round_kernel(const float *__restrict__ dh32, bf16_t *__restrict__ dh, const int32_t *__restrict__ place,
-                                                         const int32_t *__restrict__ count, int vocab, int d, int64_t ldw, int64_t most) {
+                                                         const Cut *__restrict__ cut, int d) {
   const int t = blockIdx.x, k = (blockIdx.y * 256 + threadIdx.x) * 4, r = place[t];
   if (k >= d) return;
-  const GradCut cut(*count, (vocab + TILE_V - 1) / TILE_V, d, ldw, most);
-  const int slices = cut.slices, n_pad = cut.nm * 256;
+  const int slices = cut->slices, n_pad = cut->nm * 256;
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
   if (r >= 0)
 #pragma unroll 8
@@ -572,7 +614,8 @@ struct Carver {
 };
 
 struct ForwardSpace {
-  int32_t *count, *rows;
+  Cut *cut;
+  int32_t *rows;
   Row *info;
   bf16_t *op;
   float *zt;
@@ -583,19 +626,20 @@ struct ForwardSpace {
     Carver c{(char *)ws};
     n_pad = padded(std::min(n, PIECE));
     groups = (vocab + GROUP - 1) / GROUP;
-    count = c.take<int32_t>(1); rows = c.take<int32_t>(n); info = c.take<Row>(n_pad); op = c.take<bf16_t>((int64_t)n_pad * d);
+    cut = c.take<Cut>(1); rows = c.take<int32_t>(n); info = c.take<Row>(n_pad); op = c.take<bf16_t>((int64_t)n_pad * d);
     zt = c.take<float>(n_pad); parts = c.take<float2>((int64_t)groups * n_pad);
     bytes = c.at - (char *)ws;
   }
 };
 
-// Elements of a piece's G.  More takes fewer launches whose last tiles leave units without work (7B shape, 3328
-// rows, 48 / 96 / 192 / 384 Mi: 9.79 / 8.71 / 8.49 / 8.40 ms), and memory.
-constexpr int64_t GRAD_MOST = (int64_t)192 << 20;
+// Tiles of 256 x 256 of a piece's G.  More takes fewer launches whose last tiles leave units without work (7B shape, 3328
+// rows, about 750 / 1500 / 3000 / 6000 of them: 9.79 / 8.71 / 8.49 / 8.40 ms), and memory.
+constexpr int GRAD_MOST = 3000;
 constexpr int NUMBER_MOST = 1024;   // positions that the gather's workgroups number for themselves
 
 struct GradSpace {
-  int32_t *count, *tickets, *rows, *place;
+  Cut *cut;
+  int32_t *tickets, *rows, *place;
   Row *info;
   bf16_t *op, *turned, *G;
   float *dh32;
@@ -607,11 +651,10 @@ struct GradSpace {
     // the most that any number of rows asks for
     int64_t g = 0, sums = 0;
     for (int rows = 256; rows <= n_pad; rows += 256) {
-      const GradCut cut(rows, (vocab + TILE_V - 1) / TILE_V, d, d, GRAD_MOST);
-      g = std::max(g, (int64_t)rows * cut.piece * TILE_V);
-      sums = std::max(sums, (int64_t)rows * cut.slices_most);
+      g = std::max(g, (int64_t)rows * Cut::of(rows, vocab, d, d, GRAD_MOST).piece * TILE_V);
+      sums = std::max(sums, (int64_t)rows * Cut::slices_most(rows / 256, d));
     }
-    count = c.take<int32_t>(1); tickets = c.take<int32_t>(16 * 32); rows = c.take<int32_t>(n); place = c.take<int32_t>(n); info = c.take<Row>(n_pad);
+    cut = c.take<Cut>(1); tickets = c.take<int32_t>(16 * 32); rows = c.take<int32_t>(n); place = c.take<int32_t>(n); info = c.take<Row>(n_pad);
     op = c.take<bf16_t>((int64_t)n_pad * d); turned = c.take<bf16_t>((int64_t)n_pad * d);
     G = c.take<bf16_t>(g);
     dh32 = c.take<float>(sums * d);
@@ -623,14 +666,14 @@ int grad_pieces(int n_pad, int vocab, int d, int64_t ldw) {
   const int v_tiles = (vocab + TILE_V - 1) / TILE_V;
   int most = 1;
   for (int rows = 256; rows <= n_pad; rows += 256) {
-    const GradCut cut(rows, v_tiles, d, ldw, GRAD_MOST);
-    most = std::max(most, (v_tiles + cut.piece - 1) / cut.piece);
+    const int piece = Cut::of(rows, vocab, d, ldw, GRAD_MOST).piece;
+    most = std::max(most, (v_tiles + piece - 1) / piece);
   }
   return most;
 }
 
 // Calls f(a kernel's shape as constants, workgroups) for logits of up to n rows.  Few rows stream W: tiles of 128 entries, of which two are on a unit and
-// the last ones leave fewer units without work than 256 of them do (1.5B shape, 61 positions: @NARROW@).
+// the last ones leave fewer units without work than 256 of them do (1.5B shape, 61 positions: 110 -> 96 us).
 template <typename F>
 void with_shape(int n, F f) {
   using std::integral_constant;
@@ -645,19 +688,28 @@ int64_t token_logprob_workspace_bytes(int n, int vocab, int d) { return ForwardS
 
 int launch_token_logprob(const TokenLoss &p, float *logprob, float *lse, hipStream_t s) {
   const ForwardSpace w(p.workspace, p.n, p.vocab, p.d);
-  const Head q{p.h, p.w, p.ldh, p.ldw, p.target, p.inv_t, nullptr, nullptr, w.rows, w.count, p.vocab, p.d};
-  const Positions at{p.target, w.count, w.rows, nullptr, logprob, lse, p.n, p.vocab};
+  const Head q{p.h, p.w, p.ldh, p.ldw, p.target, p.inv_t, nullptr, nullptr, w.rows, w.cut, p.vocab, p.d};
+  const Positions at{p.target, w.cut, w.rows, nullptr, logprob, lse, p.n, p.vocab, p.d, GRAD_MOST, p.ldw};
   const bool number = p.n <= NUMBER_MOST;
+  auto merge = [&](int first) {
+    hipLaunchKernelGGL(loss_merge_kernel, dim3((std::min(p.n - first, w.n_pad) + JOIN_ROWS - 1) / JOIN_ROWS), dim3(1024), 0, s, w.parts, w.zt, w.rows, w.cut, logprob, lse,
+                       w.groups, first, w.n_pad);
+  };
+  if (p.n <= DIRECT_MOST && (p.n * p.ldh + p.d) * 2 < 0x7fff0000) {   // (rows behind one 32-bit offset)
+    hipLaunchKernelGGL((loss_forward_kernel<2, 2, 2, 1, true, true>), dim3(2 * UNITS), dim3(256), 0, s, q, at, w.op, w.info, w.parts, w.zt, 0, w.n_pad);
+    merge(0);
+    return done();
+  }
   if (!number) hipLaunchKernelGGL(loss_rows_kernel, dim3(1), dim3(1024), 0, s, at);
   for (int first = 0; first < p.n; first += PIECE) {
     auto gather = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(w.n_pad / 32, p.d / 64), dim3(256), 0, s, q, at, first, w.op, (bf16_t *)nullptr, w.info); };
     if (number) gather(loss_gather_kernel<true>); else gather(loss_gather_kernel<false>);
     with_shape(std::min(p.n - first, PIECE), [&](auto WM, auto WN, auto AT, auto BT, int grid) {
-      auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, s, q, w.op, w.info, w.parts, w.zt, first, w.n_pad); };
+      auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, s, q, at, w.op, w.info, w.parts, w.zt, first, w.n_pad); };
       constexpr bool once = WM.value > 1;   // (tiles of up to 128 rows: there is one of them)
-      launch(loss_forward_kernel<WM.value, WN.value, AT.value, BT.value, once>);
+      launch(loss_forward_kernel<WM.value, WN.value, AT.value, BT.value, once, false>);
     });
-    hipLaunchKernelGGL(loss_merge_kernel, dim3((std::min(p.n - first, w.n_pad) + JOIN_ROWS - 1) / JOIN_ROWS), dim3(1024), 0, s, w.parts, w.zt, w.rows, w.count, logprob, lse, w.groups, first, w.n_pad);
+    merge(first);
   }
   return done();
 }
@@ -666,8 +718,8 @@ int64_t token_logprob_grad_workspace_bytes(int n, int vocab, int d) { return Gra
 
 int launch_token_logprob_grad(const TokenLoss &p, const float *lse, const float *g, bf16_t *dh, bf16_t *dw, hipStream_t s) {
   const GradSpace w(p.workspace, p.n, p.vocab, p.d);
-  const Head q{p.h, p.w, p.ldh, p.ldw, p.target, p.inv_t, lse, g, w.rows, w.count, p.vocab, p.d};
-  const Positions at{p.target, w.count, w.rows, w.place, nullptr, nullptr, p.n, p.vocab};
+  const Head q{p.h, p.w, p.ldh, p.ldw, p.target, p.inv_t, lse, g, w.rows, w.cut, p.vocab, p.d};
+  const Positions at{p.target, w.cut, w.rows, w.place, nullptr, nullptr, p.n, p.vocab, p.d, GRAD_MOST, p.ldw};
   const bool number = p.n <= NUMBER_MOST;
   if (!number) hipLaunchKernelGGL(loss_rows_kernel, dim3(1), dim3(1024), 0, s, at);
   auto gather = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(w.n_pad / 32, p.d / 64), dim3(256), 0, s, q, at, 0, w.op, w.turned, w.info); };
@@ -675,14 +727,13 @@ int launch_token_logprob_grad(const TokenLoss &p, const float *lse, const float 
   const int pieces = grad_pieces(w.n_pad, p.vocab, p.d, p.ldw);
   with_shape(p.n, [&](auto WM, auto WN, auto AT, auto BT, int grid) {
     for (int i = 0; i < pieces; ++i) {
-      hipLaunchKernelGGL((loss_grad_logits_kernel<WM.value, WN.value, AT.value, BT.value>), dim3(grid), dim3(256), 0, s, q, w.op, w.info, w.G, i, GRAD_MOST,
-                         w.n_pad, w.tickets);
-      const GradParams gp{w.G, w.turned, dh ? w.dh32 : nullptr, dw, w.tickets, GRAD_MOST, i, w.n_pad, WN.value * BT.value * 32};
+      hipLaunchKernelGGL((loss_grad_logits_kernel<WM.value, WN.value, AT.value, BT.value>), dim3(grid), dim3(256), 0, s, q, w.op, w.info, w.G, i, w.n_pad, w.tickets);
+      const GradParams gp{w.G, w.turned, dh ? w.dh32 : nullptr, dw, w.tickets, i, w.n_pad, WN.value * BT.value * 32};
       hipLaunchKernelGGL(loss_grad_kernel, dim3(UNITS), dim3(256), 0, s, q, gp);
     }
   });
   if (dh)
-    hipLaunchKernelGGL(loss_round_kernel, dim3(p.n, (p.d / 4 + 255) / 256), dim3(256), 0, s, w.dh32, dh, w.place, w.count, p.vocab, p.d, p.ldw, GRAD_MOST);
+    hipLaunchKernelGGL(loss_round_kernel, dim3(p.n, (p.d / 4 + 255) / 256), dim3(256), 0, s, w.dh32, dh, w.place, w.cut, p.d);
   return done();
 }
 
