@@ -109,9 +109,10 @@ struct Head {
 };
 
 // Rows [first, first + 32 * gridDim.x) in operand order (planes of 64 k, blocks of 32 rows; padding 0), their transpose in operand order (if any: planes
-// of 64 rows, blocks of 32 k), and what the tiles want to know of each.  NUMBER: few positions, which every workgroup numbers for itself instead of a launch ahead.
+// of 64 rows, blocks of 32 k; `low`: rows below it a second time, so many rows on), and what the tiles want to know of each.  NUMBER: few positions, which every workgroup numbers for itself instead of a launch ahead.
 template <bool NUMBER>
-__global__ __launch_bounds__(256) void loss_gather_kernel(Head q, Positions at, int first, bf16_t *__restrict__ op, bf16_t *__restrict__ turned, Row *__restrict__ info) {
+__global__ __launch_bounds__(256) void loss_gather_kernel(Head q, Positions at, int first, bf16_t *__restrict__ op, bf16_t *__restrict__ turned, int low,
+                                                          Row *__restrict__ info) {
   const int r0 = blockIdx.x * 32, j = threadIdx.x >> 6, half = (threadIdx.x >> 5) & 1, r = r0 + (threadIdx.x & 31), k = blockIdx.y * 64 + half * 32 + j * 8;
   int t = -1;
   if constexpr (NUMBER) {
@@ -130,7 +131,7 @@ __global__ __launch_bounds__(256) void loss_gather_kernel(Head q, Positions at, 
   }
   const uint4 v = t >= 0 ? *(const uint4 *)(q.h + t * q.ldh + k) : make_uint4(0, 0, 0, 0);
   *(uint4 *)(op + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 2048 + threadIdx.x * 8) = v;
-  if (turned) {   // (uniform)
+  if (turned && (low == 0 || r0 < low)) {   // (uniform)
     __shared__ __attribute__((aligned(16))) bf16_t block[32][72];
     *(uint4 *)&block[threadIdx.x & 31][half * 32 + j * 8] = v;
     __syncthreads();
@@ -139,7 +140,8 @@ __global__ __launch_bounds__(256) void loss_gather_kernel(Head q, Positions at, 
 #pragma unroll
     for (int e = 0; e < 8; ++e) o[e] = block[j * 8 + e][c];
     const int k32 = (blockIdx.y * 64 + c) >> 5;
-    *(bf16x8 *)(turned + ((((int64_t)(r0 >> 6) * (q.d >> 5) + k32) * 4 + j) * 64 + ((r0 >> 5) & 1) * 32 + (c & 31)) * 8) = o;
+    for (int to = r0; to <= r0 + low; to += low ? low : 1)
+      *(bf16x8 *)(turned + ((((int64_t)(to >> 6) * (q.d >> 5) + k32) * 4 + j) * 64 + ((to >> 5) & 1) * 32 + (c & 31)) * 8) = o;
   }
   if (blockIdx.y == 0 && threadIdx.x < 32) {
     Row i{0.f, 0.f, 0.f, -1};
@@ -350,18 +352,25 @@ __device__ __forceinline__ int64_t fragment_place(int row, int k32, int n, int f
   return ((((int64_t)(k32 >> 1) * (n >> 5) + row) * 4 + 2 * f + half) * 64 + (k32 & 1) * 32 + lrow) * 16;
 }
 
-// G of a piece of the vocabulary, in operand order (a row's entries are its k; rows to whole tiles).  Clears the tickets of the kernel behind.
+// Few rows: one tile of them, and G in two terms.  A product of bf16 operands rounds each entry of G by up to 2^-8, and where the sums are of few
+// large entries nothing averages that out; the remainders, as so many rows more, fill k-steps and columns that would be padding.  (Error of dh and dW
+// over that of their own rounding, 33 positions: 1.15 to 1.63 -> 1.00.)
+constexpr int SPLIT_MOST = 128;
+
+// G of a piece of the vocabulary, in operand order (a row's entries are its k; rows to whole tiles, then those of the remainders).  Clears the tickets of the
+// kernel behind.
 template <int WM, int WN, int AT, int BT>
 __global__ __launch_bounds__(256) void loss_grad_logits_kernel(Head q, const bf16_t *__restrict__ op, const Row *__restrict__ info, bf16_t *__restrict__ G_out,
                                                                int index, int n_pad, int32_t *__restrict__ tickets) {
   typedef Tile<WM, WN, AT, BT, false, TILE_COLS> T;
+  constexpr bool SPLIT = T::BN <= SPLIT_MOST;
   __shared__ __attribute__((aligned(1024))) bf16_t xs[T::LDS];
   if (blockIdx.x == 0 && threadIdx.x < 16) tickets[threadIdx.x * 32] = 0;
   const Cut cut = *q.cut;
   const int count = cut.count;
   const int64_t begin = (int64_t)index * cut.piece * TILE_V;
   if (begin >= q.vocab) return;
-  const int v_begin = (int)begin, width = cut.piece * TILE_V, n_rows = (count + T::BN - 1) / T::BN * T::BN;
+  const int v_begin = (int)begin, width = cut.piece * TILE_V, n_rows = SPLIT ? 2 * T::BN : (count + T::BN - 1) / T::BN * T::BN;
   LogitTiles<T::BM, T::BN> tiles;
   tiles.init(count, min(width, (q.vocab - v_begin + TILE_V - 1) / TILE_V * TILE_V));   // (zeros behind the vocabulary, to a whole tile of the products)
   if (tiles.at >= tiles.end) return;
@@ -400,6 +409,13 @@ __global__ __launch_bounds__(256) void loss_grad_logits_kernel(Head q, const bf1
         fragments(f, G);
 #pragma unroll
         for (int k = 0; k < 2; ++k) *(uint4 *)((char *)G_out + fragment_place(m32, v32, n_rows, k, t.half, t.lrow)) = f[k];
+        if constexpr (SPLIT) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) G[i] -= (float)(bf16_t)G[i];
+          fragments(f, G);
+#pragma unroll
+          for (int k = 0; k < 2; ++k) *(uint4 *)((char *)G_out + fragment_place(m32 + T::BN / 32, v32, n_rows, k, t.half, t.lrow)) = f[k];
+        }
 #ifdef __HIP_DEVICE_COMPILE__
         __builtin_amdgcn_sched_barrier(0);   // (one block's registers at a time)
 #endif
@@ -413,7 +429,7 @@ struct GradParams {
   float *dh32;                              // [slices][rows, to a multiple of 256][d], or null: no dh
   bf16_t *dw;                               // or null
   int32_t *tickets;                         // sixteen, 128 bytes apart, zero: eight of each kind of tile
-  int index, n_pad, tile_rows;              // the piece; rows of `turned`; rows of a tile of the kernel that made G
+  int index, tile_rows, low;                // the piece; rows of a tile of the kernel that made G; where the remainders' rows begin, or 0: none
 };
 
 // Tiles that the units take by tickets, from their own XCD's eighth and, when that is done, from the others'.  The first ones are dealt without a ticket,
@@ -491,7 +507,7 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(Head q, GradParams g) {
   const int64_t begin = (int64_t)g.index * cut.piece * TILE_V;
   if (begin >= q.vocab) return;
   const int v_begin = (int)begin, nm = cut.nm, nv = min(cut.piece, (q.vocab - v_begin + TILE_V - 1) / TILE_V), n_rows = nm * 256;
-  const int g_rows = (count + g.tile_rows - 1) / g.tile_rows * g.tile_rows;   // of G
+  const int g_rows = g.low ? 2 * g.low : (count + g.tile_rows - 1) / g.tile_rows * g.tile_rows;   // of G
   const int64_t g_plane = (int64_t)g_rows * 64;
   const int k_all = nv * (TILE_V / BK), k_slice = cut.slice * (TILE_V / BK);
   // the walk over one kind of tile
@@ -530,7 +546,7 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(Head q, GradParams g) {
       for (int b = 0; b < 2; ++b) {
         const int r = c.row0 + (t.wn * 2 + b) * 32 + t.lrow;
         float *o = g.dh32 + ((int64_t)c.kind * n_rows + r) * q.d + c.col0 + t.half * 4;
-        if (r < count) {
+        if (r < count || (g.low && r >= g.low && r - g.low < count)) {
 #pragma unroll
           for (int a = 0; a < 8; ++a) {
             f32x4 sum[4];
@@ -583,16 +599,19 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(Head q, GradParams g) {
   }
 }
 
-// dh of every position: the slices of its row added up in order and rounded, or zeros
+// dh of every position: the slices of its row (and of its remainders' row) added up in order and rounded, or zeros
 __global__ __launch_bounds__(256) void loss_round_kernel(const float *__restrict__ dh32, bf16_t *__restrict__ dh, const int32_t *__restrict__ place,
-                                                         const Cut *__restrict__ cut, int d) {
+                                                         const Cut *__restrict__ cut, int d, int low) {
   const int t = blockIdx.x, k = (blockIdx.y * 256 + threadIdx.x) * 4, r = place[t];
   if (k >= d) return;
   const int slices = cut->slices, n_pad = cut->nm * 256;
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
   if (r >= 0)
+    for (int rest = 0; rest <= low; rest += low ? low : 1) {   // (the remainders' row)
+      const float *at = dh32 + (int64_t)(r + rest) * d + k;
 #pragma unroll 8
-    for (int s = 0; s < slices; ++s) v += *(const f32x4 *)(dh32 + ((int64_t)s * n_pad + r) * d + k);
+      for (int s = 0; s < slices; ++s) v += *(const f32x4 *)(at + (int64_t)s * n_pad * d);
+    }
   bf16x4 o;
 #pragma unroll
   for (int e = 0; e < 4; ++e) o[e] = (bf16_t)v[e];
@@ -702,7 +721,7 @@ int launch_token_logprob(const TokenLoss &p, float *logprob, float *lse, hipStre
   }
   if (!number) hipLaunchKernelGGL(loss_rows_kernel, dim3(1), dim3(1024), 0, s, at);
   for (int first = 0; first < p.n; first += PIECE) {
-    auto gather = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(w.n_pad / 32, p.d / 64), dim3(256), 0, s, q, at, first, w.op, (bf16_t *)nullptr, w.info); };
+    auto gather = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(w.n_pad / 32, p.d / 64), dim3(256), 0, s, q, at, first, w.op, (bf16_t *)nullptr, 0, w.info); };
     if (number) gather(loss_gather_kernel<true>); else gather(loss_gather_kernel<false>);
     with_shape(std::min(p.n - first, PIECE), [&](auto WM, auto WN, auto AT, auto BT, int grid) {
       auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, s, q, at, w.op, w.info, w.parts, w.zt, first, w.n_pad); };
@@ -720,20 +739,21 @@ int launch_token_logprob_grad(const TokenLoss &p, const float *lse, const float 
   const GradSpace w(p.workspace, p.n, p.vocab, p.d);
   const Head q{p.h, p.w, p.ldh, p.ldw, p.target, p.inv_t, lse, g, w.rows, w.cut, p.vocab, p.d};
   const Positions at{p.target, w.cut, w.rows, w.place, nullptr, nullptr, p.n, p.vocab, p.d, GRAD_MOST, p.ldw};
+  const int low = p.n <= 64 ? 64 : p.n <= SPLIT_MOST ? SPLIT_MOST : 0;   // (a tile's rows: with_shape)
   const bool number = p.n <= NUMBER_MOST;
   if (!number) hipLaunchKernelGGL(loss_rows_kernel, dim3(1), dim3(1024), 0, s, at);
-  auto gather = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(w.n_pad / 32, p.d / 64), dim3(256), 0, s, q, at, 0, w.op, w.turned, w.info); };
+  auto gather = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(w.n_pad / 32, p.d / 64), dim3(256), 0, s, q, at, 0, w.op, w.turned, low, w.info); };
   if (number) gather(loss_gather_kernel<true>); else gather(loss_gather_kernel<false>);
   const int pieces = grad_pieces(w.n_pad, p.vocab, p.d, p.ldw);
   with_shape(p.n, [&](auto WM, auto WN, auto AT, auto BT, int grid) {
     for (int i = 0; i < pieces; ++i) {
       hipLaunchKernelGGL((loss_grad_logits_kernel<WM.value, WN.value, AT.value, BT.value>), dim3(grid), dim3(256), 0, s, q, w.op, w.info, w.G, i, w.n_pad, w.tickets);
-      const GradParams gp{w.G, w.turned, dh ? w.dh32 : nullptr, dw, w.tickets, i, w.n_pad, WN.value * BT.value * 32};
+      const GradParams gp{w.G, w.turned, dh ? w.dh32 : nullptr, dw, w.tickets, i, WN.value * BT.value * 32, low};
       hipLaunchKernelGGL(loss_grad_kernel, dim3(UNITS), dim3(256), 0, s, q, gp);
     }
   });
   if (dh)
-    hipLaunchKernelGGL(loss_round_kernel, dim3(p.n, (p.d / 4 + 255) / 256), dim3(256), 0, s, w.dh32, dh, w.place, w.cut, p.d);
+    hipLaunchKernelGGL(loss_round_kernel, dim3(p.n, (p.d / 4 + 255) / 256), dim3(256), 0, s, w.dh32, dh, w.place, w.cut, p.d, low);
   return done();
 }
 
