@@ -292,81 +292,94 @@ __global__ __launch_bounds__(256) void int8_slices_kernel(const i32x4 *__restric
   else *(uint2 *)(y + (int64_t)m * N + n) = make_uint2(two_bf16(r[0], r[1]), two_bf16(r[2], r[3]));
 }
 
-// Few rows (at most ROWS) in one launch: a workgroup quantises them for itself into LDS, under its first loads of W, and owns 32 channels. Eight wavefronts take
-// turns of 1 KiB of W (32 channels x 2 x 16 k in operand order: a lane has sixteen codes of one channel), against which each row's codes come
-// from LDS, the same for half a wavefront.  Bound by W's way from memory.
+// Few rows in one launch: a workgroup quantises them for itself into LDS, under its first loads of W, and walks blocks of 32 channels.  Its eight wavefronts
+// take turns of 1 KiB of a block of W (32 channels x 2 x 16 k in operand order: one operand of a matrix instruction, straight from memory), the other
+// operand comes from the codes in LDS; at a block's end their sums are added up in LDS.  Nothing but W's way from memory is left to bound it.
+// ROWS (1, 2, 4): 8 / ROWS wavefronts quantise a row.
+constexpr int FEW_AHEAD = 8;    // turns of a wavefront whose loads are in flight
+constexpr int FEW_HELD = 8;     // pieces of eight values that a lane holds of a row between its two looks
 template <int ROWS, typename T>
 __global__ __launch_bounds__(512) void gemm_int8_few_kernel(const bf16_t *__restrict__ x, int64_t ldx, const int8_t *__restrict__ wq, const float *__restrict__ sw, T *__restrict__ y,
                                                             int M, int N, int K) {
-  constexpr int AHEAD = 8;   // turns of a wavefront whose loads are in flight
-  extern __shared__ __attribute__((aligned(16))) int8_t codes[];   // [ROWS][K]
-  __shared__ float part[8], scale[ROWS];
-  __shared__ int32_t sums[8][ROWS][32];
-  const int l = threadIdx.x & 63, wave = threadIdx.x >> 6, turns = K >> 8;
-  const i32x4 *w = (const i32x4 *)(wq + ((int64_t)(wave >> 2) * (N >> 5) + blockIdx.x) * 4096 + (wave & 3) * 1024) + l;
-  const int64_t step = (int64_t)N * 16;   // 256 k on, in vectors
-  i32x4 cur[AHEAD], nxt[AHEAD];
+  extern __shared__ __attribute__((aligned(16))) int8_t few_lds[];
+  // scales and maxima, sums of the wavefronts [8][16][64], codes [M][K + 16] (16 bytes more per row: consecutive rows begin in other banks; 2 KB behind
+  // the last row are read against zeros)
+  float *scale = (float *)few_lds, *part = scale + 8;
+  int32_t *sums = (int32_t *)(few_lds + 256);
+  int8_t *codes = few_lds + 256 + 8 * 4096;
+  const int l = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), turns = K >> 8, pitch = K + 16, blocks = N >> 5;
+  // The turns of a wavefront, block after block, as one sequence: of each block a multiple of FEW_AHEAD, those behind K reading as zeros (they lie behind
+  // the end of W).  A turn's registers are filled for the turn FEW_AHEAD on as soon as it is done.
+  const int turns_pad = (turns + FEW_AHEAD - 1) / FEW_AHEAD * FEW_AHEAD, step = N * 256;   // (bytes: 256 k on)
+  const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc((void *)wq, 0, (int)((int64_t)N * K), 0x00020000);
+  const int first = __builtin_amdgcn_readfirstlane((wave >> 2) * N * 128 + (wave & 3) * 1024);
+  auto load = [&](int block, int t) {
+    return __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, l * 16, (int)((uint32_t)first + (uint32_t)block * 4096u + (uint32_t)t * (uint32_t)step), 2));
+  };
+  i32x4 cur[FEW_AHEAD];
 #pragma unroll
-  for (int u = 0; u < AHEAD; ++u)
-    if (u < turns) cur[u] = __builtin_nontemporal_load(w + u * step);
+  for (int u = 0; u < FEW_AHEAD; ++u) cur[u] = load(blockIdx.x, u);
 
-  // wavefronts share the rows: 512 / ROWS lanes each
-  constexpr int WAVES = 8 / ROWS;
-  const int pieces = K >> 3, row = wave / WAVES, first = threadIdx.x & (64 * WAVES - 1);
-  x += min(row, M - 1) * ldx;
-  Values<bf16_t, 8> v;
-  float m = 0.f;
-  for (int p = first; p < pieces; p += 64 * WAVES) {
-    v.load(x + p * 8);
-    m = v.most(m);
-  }
-  m = wave_max(m);
-  if (l == 0) part[wave] = m;
-  __syncthreads();
+  {
+    constexpr int WAVES = 8 / ROWS, LANES = 64 * WAVES;
+    const int row = wave / WAVES, at = threadIdx.x & (LANES - 1), pieces = K >> 3;   // (a row beyond M: the last one again, into no one's place)
+    const bf16_t *mine = x + min(row, M - 1) * ldx;
+    Values<bf16_t, 8> v[FEW_HELD];
+    float m = 0.f;
 #pragma unroll
-  for (int i = 0; i < WAVES; ++i) m = fmaxf(m, part[row * WAVES + i]);
-  const RowScale rs(m);
-  if (first == 0) scale[row] = rs.scale;
-  for (int p = first; p < pieces; p += 64 * WAVES) {
-    if (pieces > 64 * WAVES) v.load(x + p * 8);
-    uint32_t c[2];
-    v.codes(rs, c);
-    *(uint2 *)(codes + row * K + p * 8) = make_uint2(c[0], c[1]);
-  }
-  __syncthreads();
-
-  int32_t sum[ROWS];
+    for (int u = 0; u < FEW_HELD; ++u)
+      if (at + u * LANES < pieces) v[u].load(mine + (at + u * LANES) * 8);
 #pragma unroll
-  for (int r = 0; r < ROWS; ++r) sum[r] = 0;
-  const int8_t *mine = codes + (wave >> 2) * 128 + (l >> 5) * 64 + (wave & 3) * 16;
-  for (int t0 = 0; t0 < turns; t0 += AHEAD) {
+    for (int u = 0; u < FEW_HELD; ++u)
+      if (at + u * LANES < pieces) m = v[u].most(m);
+    m = wave_max(m);
+    if (l == 0) part[wave] = m;
+    __syncthreads();
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u)
-      if (t0 + AHEAD + u < turns) nxt[u] = __builtin_nontemporal_load(w + (t0 + AHEAD + u) * step);
+    for (int i = 0; i < WAVES; ++i) m = fmaxf(m, part[row * WAVES + i]);
+    const RowScale rs(m);
+    if (at == 0 && row < M) scale[row] = rs.scale;
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u)
-      if (t0 + u < turns) {
-#pragma unroll
-        for (int r = 0; r < ROWS; ++r) {
-          const i32x4 c = *(const i32x4 *)(mine + r * K + (t0 + u) * 256);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) sum[r] = __builtin_amdgcn_sdot4(cur[u][e], c[e], sum[r], false);
-        }
+    for (int u = 0; u < FEW_HELD; ++u)
+      if (at + u * LANES < pieces && row < M) {
+        uint32_t c[2];
+        v[u].codes(rs, c);
+        *(uint2 *)(codes + row * pitch + (at + u * LANES) * 8) = make_uint2(c[0], c[1]);
       }
-#pragma unroll
-    for (int u = 0; u < AHEAD; ++u) cur[u] = nxt[u];
+    __syncthreads();
   }
+
+  const int8_t *mine = codes + min(l & 31, M - 1) * pitch + (wave >> 2) * 128 + (l >> 5) * 64 + (wave & 3) * 16;
+  for (int block = blockIdx.x; block < blocks; block += gridDim.x) {
+    i32x16 sum;
 #pragma unroll
-  for (int r = 0; r < ROWS; ++r) {
-    sum[r] = with_xor32(sum[r], [](int a, int b) { return a + b; });
-    if (l < 32) sums[wave][r][l] = sum[r];
+    for (int i = 0; i < 16; ++i) sum[i] = 0;
+    for (int t0 = 0; t0 < turns_pad; t0 += FEW_AHEAD) {
+      const bool last = t0 + FEW_AHEAD == turns_pad;
+      const int block_on = last ? min(block + (int)gridDim.x, blocks - 1) : block, t_on = last ? 0 : t0 + FEW_AHEAD;   // (behind the last block: any)
+#pragma unroll
+      for (int u = 0; u < FEW_AHEAD; ++u) {
+#ifdef __HIP_DEVICE_COMPILE__
+        sum = __builtin_amdgcn_mfma_i32_32x32x32_i8(cur[u], *(const i32x4 *)(mine + (t0 + u) * 256), sum, 0, 0, 0);
+#endif
+        cur[u] = load(block_on, t_on + u);
+      }
+    }
+    // sums of a wavefront: register i of lane l is channel (i / 4) * 8 + (l / 32) * 4 + i % 4, row l % 32
+    if ((l & 31) < ROWS) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sums[(wave * 16 + i) * 64 + l] = sum[i];
+    }
+    __syncthreads();
+    if (threadIdx.x < 32 * ROWS) {
+      const int r = threadIdx.x & (ROWS - 1), c = threadIdx.x / ROWS, i = (c >> 3) * 4 + (c & 3), n = block * 32 + c;   // (c: channel)
+      int32_t s = 0;
+#pragma unroll
+      for (int w = 0; w < 8; ++w) s += sums[(w * 16 + i) * 64 + ((c >> 2) & 1) * 32 + r];
+      if (r < M) y[(int64_t)r * N + n] = (T)((float)s * scale[r] * sw[n]);
+    }
+    __syncthreads();
   }
-  __syncthreads();
-  const int r = threadIdx.x >> 5, n = blockIdx.x * 32 + (threadIdx.x & 31);
-  if (r >= ROWS || r >= M) return;
-  int32_t s = 0;
-  for (int i = 0; i < 8; ++i) s += sums[i][r][threadIdx.x & 31];
-  y[(int64_t)r * N + n] = (T)((float)s * scale[r] * sw[n]);
 }
 
 int done() { return hipGetLastError() == hipSuccess ? 0 : -7; }
@@ -376,16 +389,26 @@ int64_t align256(int64_t b) { return (b + 255) / 256 * 256; }
 // more * (average beyond one workgroup per unit) + round * (workgroups of the fullest unit - 1)), out per MB of bf16 results, and with slices their
 // launch and MB of sums.  Fitted to 2700 launches (the products of the 1.5B, 7B and 32B shapes and smaller ones, 1 to 3001 rows, 1 to 24 slices, weights
 // not in the last-level cache): the choice takes 1.2 % more than the best measured one on average, 6 % in 95 of 100.
-enum { I8_32x128, I8_64x128, I8_128x128, I8_128x256, I8_64x64, I8_ROUNDS };
+enum { I8_32x128, I8_64x128, I8_128x128, I8_128x256, I8_64x64, I8_ROUNDS, I8_FEW };
 struct ShapeTime { int rows, cols; float fixed, base, load, more, round, slices, slice_mb, out_mb; };
 constexpr ShapeTime SHAPES[] = {{32, 128, 5.29f, 0.275f, 0.137f, 0.128f, 0.217f, 4.46f, 0.203f, 0.f},   {64, 128, 5.88f, 0.324f, 0.197f, 0.155f, 0.25f, 3.67f, 0.371f, 0.f},
                                 {128, 128, 7.75f, 0.359f, 0.289f, 0.278f, 0.313f, 2.88f, 0.386f, 0.098f}, {128, 256, 8.39f, 0.625f, 0.623f, 0.419f, 0.707f, 2.75f, 0.337f, 0.067f},
                                 {64, 64, 5.53f, 0.21f, 0.117f, 0.123f, 0.17f, 2.6f, 0.434f, 0.f},          {256, 256, 21.f, 0.98f, 0.393f, 0.407f, 1.258f, 0.f, 0.f, 0.377f}};
 struct Int8Plan { int shape, splits, slice; };
+// gemm_int8_few_kernel, where a workgroup holds its rows in registers while it looks for their largest magnitudes: fixed (less 2 for the launches that the
+// caller's thread does not make), the quantisation, and a workgroup's part of W at what a unit gets, or all of W.  us, measured so / in two launches: 1 row 3584 x 3584 7.5 / 10.4, 37888 x 3584 22.9 / 28.8, 1536 x 8960
+// 12.3 / 11.1, 5120 x 27648 26.6 / 29.0; 4 rows 3584 x 3584 9.4 / 10.7, 37888 x 3584 23.5 / 29.0; 8 rows (a wavefront each) 16.2 / 11.2 and 29.1 / 30.4.
+int few_rows(int M) { return M > 2 ? 4 : M; }
+bool few_fits(int M, int K) { return M <= 4 && few_rows(M) * K <= 512 * FEW_HELD * 8; }
+float few_us(int M, int N, int K) {
+  const float rounds = (N / 32 + 2 * UNITS - 1) / (2 * UNITS);
+  return std::max(2.8f + 1.5e-4f * few_rows(M) * K + rounds * K * (32 / 45e3f), 1.f + (float)N * K * (1 / 6.4e6f));
+}
 Int8Plan int8_plan(int M, int N, int K) {
   const int groups = (K + K_UNIT - 1) / K_UNIT;
-  const float mb = 1e-6f * M * N;
+  const float mb = 1e-6f * M * N, few = few_fits(M, K) ? few_us(M, N, K) : 1e30f;
   Int8Plan best{-1, 1, 0};
+  if (few < 8) return Int8Plan{I8_FEW, 1, 0};   // (two launches take no less)
   float best_us = 0;
   for (int shape = 0; shape <= I8_ROUNDS; ++shape) {
     const ShapeTime &f = SHAPES[shape];
@@ -405,15 +428,8 @@ Int8Plan int8_plan(int M, int N, int K) {
       }
     }
   }
+  if (few < best_us) best = Int8Plan{I8_FEW, 1, 0};
   return best;
-}
-
-// Calls of gemm_int8_few_kernel.  What every workgroup does for itself grows with rows x K and with the number of workgroups: us, in one launch / in
-// two, 1 row 4608 x 3584 6.6 / 10.7, 37888 x 3584 26.9 / 29.6, 55296 x 5120 46.4 / 44.9, 3584 x 18944 20.2 / 19.1; 2 rows 4608 x 3584 7.7 / 11.0, 1536 x
-// 8960 14.7 / 11.2; 4 rows 4608 x 3584 8.8 / 10.5, 17920 x 1536 11.1 / 10.0; tiny shape 4.5 / 7.0.
-bool int8_few(int M, int N, int K) {
-  const int rows = M > 2 ? 4 : M;
-  return M <= 4 && rows * K <= 16384 && rows * N <= 45000;
 }
 
 template <int WM, int WN, int AT, int BT>
@@ -452,18 +468,21 @@ int64_t gemm_int8_workspace_bytes(int M, int N, int K) {
 }
 
 int launch_gemm_int8(const bf16_t *x, int64_t ldx, const int8_t *wq, const float *sw, void *y, bool f32, int M, int N, int K, void *ws, hipStream_t s) {
-  if (int8_few(M, N, K)) {
-    auto launch = [&](auto kernel, auto *out) { hipLaunchKernelGGL(kernel, dim3(N / 32), dim3(512), (M > 2 ? 4 : M) * K, s, x, ldx, wq, sw, out, M, N, K); };
+  const Int8Plan plan = int8_plan(M, N, K);
+  if (plan.shape == I8_FEW) {
+    const int bytes = 256 + 8 * 4096 + M * (K + 16) + FEW_AHEAD * 256, grid = std::min(N / 32, 2 * UNITS);
+    auto launch = [&](auto kernel, auto *out) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(512), bytes, s, x, ldx, wq, sw, out, M, N, K); };
     auto with = [&](auto *out) {
       typedef std::remove_pointer_t<decltype(out)> T;
-      if (M == 1) launch(gemm_int8_few_kernel<1, T>, out);
-      else if (M == 2) launch(gemm_int8_few_kernel<2, T>, out);
-      else launch(gemm_int8_few_kernel<4, T>, out);
+      switch (few_rows(M)) {
+        case 1: launch(gemm_int8_few_kernel<1, T>, out); break;
+        case 2: launch(gemm_int8_few_kernel<2, T>, out); break;
+        default: launch(gemm_int8_few_kernel<4, T>, out);
+      }
     };
     if (f32) with((float *)y); else with((bf16_t *)y);
     return done();
   }
-  const Int8Plan plan = int8_plan(M, N, K);
   const int k_pad = (K + K_UNIT - 1) / K_UNIT * K_UNIT;
   float *sx = (float *)ws;
   int8_t *xq = (int8_t *)ws + align256((int64_t)M * 4);
