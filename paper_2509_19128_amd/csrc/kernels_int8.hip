@@ -308,13 +308,13 @@ __global__ __launch_bounds__(512) void gemm_int8_few_kernel(const bf16_t *__rest
   int32_t *sums = (int32_t *)(few_lds + 256);
   int8_t *codes = few_lds + 256 + 8 * 4096;
   const int l = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), turns = K >> 8, pitch = K + 16, blocks = N >> 5;
-  // The turns of a wavefront, block after block, as one sequence: of each block a multiple of FEW_AHEAD, those behind K reading as zeros (they lie behind
-  // the end of W).  A turn's registers are filled for the turn FEW_AHEAD on as soon as it is done.
+  // The turns of a wavefront, block after block, as one sequence: of each block a multiple of FEW_AHEAD, those behind K reading as zeros (from behind the end
+  // of W).  A turn's registers are filled for the turn FEW_AHEAD on as soon as it is done.
   const int turns_pad = (turns + FEW_AHEAD - 1) / FEW_AHEAD * FEW_AHEAD, step = N * 256;   // (bytes: 256 k on)
   const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc((void *)wq, 0, (int)((int64_t)N * K), 0x00020000);
   const int first = __builtin_amdgcn_readfirstlane((wave >> 2) * N * 128 + (wave & 3) * 1024);
   auto load = [&](int block, int t) {
-    return __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, l * 16, (int)((uint32_t)first + (uint32_t)block * 4096u + (uint32_t)t * (uint32_t)step), 2));
+    return __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, l * 16, t < turns ? first + block * 4096 + t * step : 0x7fffffff, 2));
   };
   i32x4 cur[FEW_AHEAD];
 #pragma unroll

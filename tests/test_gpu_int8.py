@@ -155,6 +155,33 @@ def test_a_row_does_not_depend_on_the_others_and_bad_rows_stay_alone():
         assert torch.equal(part, whole[rows])
 
 
+@pytest.mark.parametrize("M", [1, 2, 3, 4, 5])
+@pytest.mark.parametrize("N,K", [(32, 256), (3584, 1792), (96, 8192), (20000, 512), (64, 16384), (32, 32768)])
+def test_few_rows_and_bad_ones_among_them(M, N, K):
+    rng = np.random.default_rng(M + N + K)
+    x, w = _inputs(rng, M, N, K)
+    x[M - 1, K - 1] = np.inf
+    if M > 2:
+        x[0] = 0.0
+        x[1] *= 1e-30
+    wq, sw = int8.quantize_rows(w)
+    # scales at any place that a float may have
+    scales = torch.zeros(N + 1, device="cuda")
+    scales[1:] = torch.from_numpy(sw)
+    for out in (torch.float32, torch.bfloat16):
+        _same(product(_bf16(x), torch.from_numpy(int8.operand_image(wq)).cuda(), scales[1:], N, out), int8.product(*int8.quantize_rows(_bf16(x)), wq, sw))
+
+
+def test_millions_of_channels():
+    """One row against a W whose turns behind K would lie beyond 32 bits: equal to the same row in a call of five, which takes other kernels."""
+    N, K = 2560000, 256
+    rng = np.random.default_rng(5)
+    x = _bf16(rng.normal(size=(5, K)))
+    image = torch.randint(-127, 128, (N * K,), device="cuda", dtype=torch.int8)
+    sw = torch.rand(N, device="cuda")
+    assert torch.equal(product(x[:1], image, sw, N)[0], product(x, image, sw, N)[0])
+
+
 def test_replays_of_a_captured_product_with_eager_calls_between():
     rng = np.random.default_rng(12)
     M, N, K = 24, 3584, 1536
