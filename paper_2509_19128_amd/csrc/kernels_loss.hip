@@ -507,7 +507,7 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(Head q, GradParams g) {
   const int64_t begin = (int64_t)g.index * cut.piece * TILE_V;
   if (begin >= q.vocab) return;
   const int v_begin = (int)begin, nm = cut.nm, nv = min(cut.piece, (q.vocab - v_begin + TILE_V - 1) / TILE_V), n_rows = nm * 256;
-  const int g_rows = g.low ? 2 * g.low : (count + g.tile_rows - 1) / g.tile_rows * g.tile_rows;   // of G
+  const int g_rows = g.low ? (count > 0 ? 2 * g.low : 0) : (count + g.tile_rows - 1) / g.tile_rows * g.tile_rows;   // of G (none: all of it reads as 0)
   const int64_t g_plane = (int64_t)g_rows * 64;
   const int k_all = nv * (TILE_V / BK), k_slice = cut.slice * (TILE_V / BK);
   // the walk over one kind of tile

@@ -184,6 +184,48 @@ def test_positions_without_a_target_whatever_they_hold(what):
         assert (got[0] == 0).all() and (got[1] == 0).all()
 
 
+@pytest.mark.parametrize("n", [1, 20, 33, 100, 128, 129, 300])
+def test_batches_without_any_target(n):
+    h, w, _, it, rng = _batch(n, 700, 256, n)
+    c = Call(np.full_like(h, np.nan), w, np.full(n, -1), it)
+    c.forward()
+    lp, lse = c.results()
+    assert (lp == 0).all() and (lse == 0).all()
+    c.backward(c.lse[:n].clone(), torch.ones(n, device="cuda"))
+    dh, dw = c.gradients()
+    assert (dh == 0).all() and (dw == 0).all()
+
+
+def test_more_positions_than_a_forward_pass_holds():
+    n, vocab, d = 9001, 300, 256
+    h, w, target, it, rng = _batch(n, vocab, d, 50, masked=0.05)   # (8551 with a target: two passes)
+    c = Call(h, w, target, it)
+    c.forward()
+    _check_forward(c, h, w, target, it)
+    g = rng.normal(size=n).astype(np.float32)
+    lse = c.lse[:n].clone()
+    c.backward(lse, torch.from_numpy(g).cuda())
+    _check_gradients(c, h, w, target, lse.cpu().numpy().astype(np.float64), g.astype(np.float64), it)
+
+
+@pytest.mark.parametrize("n,ldh,ldw", [(20, 1 << 24, 1 << 20), (200, 1 << 23, 1 << 20), (40, 1 << 25, 256), (3, 256, 1 << 20)])
+def test_rows_far_apart(n, ldh, ldw):
+    """Rows of h and w that lie gigabytes apart: places beyond 32 bits, and pieces of the vocabulary that end where 32 bits do."""
+    vocab, d = 1500, 256
+    h, w, target, it, rng = _batch(n, vocab, d, 60 + n, masked=0.1)
+    c = Call(h, w, target, it)
+    far_h, far_w = (torch.empty((len(a) - 1) * ld + d, dtype=torch.bfloat16, device="cuda") for a, ld in ((h, ldh), (w, ldw)))
+    far_h.as_strided((n, d), (ldh, 1)).copy_(c.h)
+    far_w.as_strided((vocab, d), (ldw, 1)).copy_(c.w)
+    c.args = (far_h.data_ptr(), ldh, far_w.data_ptr(), ldw, *c.args[4:])
+    c.forward()
+    _check_forward(c, h, w, target, it)
+    g = rng.normal(size=n).astype(np.float32)
+    lse = c.lse[:n].clone()
+    c.backward(lse, torch.from_numpy(g).cuda())
+    _check_gradients(c, h, w, target, lse.cpu().numpy().astype(np.float64), g.astype(np.float64), it)
+
+
 def test_a_position_does_not_depend_on_the_others():
     n, vocab, d = 400, 3000, 512
     h, w, target, it, _ = _batch(n, vocab, d, 21)
