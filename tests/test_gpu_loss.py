@@ -226,6 +226,34 @@ def test_rows_far_apart(n, ldh, ldw):
     _check_gradients(c, h, w, target, lse.cpu().numpy().astype(np.float64), g.astype(np.float64), it)
 
 
+def test_temperatures_of_zero_and_below():
+    """A zero makes all tokens equally likely; what is no temperature gives its position NaN and no other."""
+    n, vocab, d = 30, 500, 256
+    h, w, target, it, _ = _batch(n, vocab, d, 70, masked=0.0)
+    it[3], it[4], it[5] = 0.0, -1.0, np.nan
+    c = Call(h, w, target, it)
+    c.forward()
+    lp, lse = c.results()
+    bad = np.isin(np.arange(n), (4, 5))
+    assert np.isnan(lp[bad]).all() and np.isnan(lse[bad]).all() and np.isfinite(lp[~bad]).all()
+    assert abs(lp[3] + np.log(vocab)) < 1e-5
+
+
+@pytest.mark.parametrize("n", [1, 30, 60, 100, 300])
+@pytest.mark.parametrize("vocab", [1, 500, 512])
+def test_inverse_temperatures_of_zero(n, vocab):
+    h, w, target, it, rng = _batch(n, vocab, 256, 80 + n + vocab, masked=0.0)
+    it[::3] = 0.0
+    c = Call(h, w, target, it)
+    c.forward()
+    _check_forward(c, h, w, target, it)
+    g = rng.normal(size=n).astype(np.float32)
+    lse = c.lse[:n].clone()
+    c.backward(lse, torch.from_numpy(g).cuda())
+    _check_gradients(c, h, w, target, lse.cpu().numpy().astype(np.float64), g.astype(np.float64), it)
+    assert (c.gradients()[0][::3] == 0).all()
+
+
 def test_a_position_does_not_depend_on_the_others():
     n, vocab, d = 400, 3000, 512
     h, w, target, it, _ = _batch(n, vocab, d, 21)
