@@ -127,6 +127,8 @@ struct Tile {
   // W_ROWS: the rows within `bytes` from W on; row b of the lane at element `at` (negative: none, zeros)
   __device__ __forceinline__ void rows_w(const bf16_t *W, int bytes) { rw = __builtin_amdgcn_make_buffer_rsrc((void *)W, 0, bytes, 0x00020000); }
   __device__ __forceinline__ void row_w(int b, int at) { w_lane[b] = at < 0 ? 0x7fff0000 : at * 2 + half * 64; }
+  // (What lies beyond an operand reads as 0 by the check of its resource's size, which takes lane and scalar offset together, a scalar offset beyond the
+  // size too: measured for sizes from 0 to 2 GiB, into registers and into LDS.)
   // x: rows (TILE_COLS_T: k) ldx elements apart from X on, of which `rows` exist (further ones read as 0); TILE_ROWS_T: an image of ldx rows, from the plane at
   // X on, of which `rows` planes of 64 exist;
   // w: operand-ordered, `n` of its rows per plane and `planes` k-steps from W on (further ones read as 0), the tile's from w_row on.

@@ -308,13 +308,13 @@ __global__ __launch_bounds__(512) void gemm_int8_few_kernel(const bf16_t *__rest
   int32_t *sums = (int32_t *)(few_lds + 256);
   int8_t *codes = few_lds + 256 + 8 * 4096;
   const int l = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), turns = K >> 8, pitch = K + 16, blocks = N >> 5;
-  // The turns of a wavefront, block after block, as one sequence: of each block a multiple of FEW_AHEAD, those behind K reading as zeros (from behind the end
-  // of W).  A turn's registers are filled for the turn FEW_AHEAD on as soon as it is done.
+  // The turns of a wavefront, block after block, as one sequence: of each block a multiple of FEW_AHEAD, those behind K reading as zeros (2 GiB on,
+  // behind the end of any W).  A turn's registers are filled for the turn FEW_AHEAD on as soon as it is done.
   const int turns_pad = (turns + FEW_AHEAD - 1) / FEW_AHEAD * FEW_AHEAD, step = N * 256;   // (bytes: 256 k on)
   const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc((void *)wq, 0, (int)((int64_t)N * K), 0x00020000);
   const int first = __builtin_amdgcn_readfirstlane((wave >> 2) * N * 128 + (wave & 3) * 1024);
   auto load = [&](int block, int t) {
-    return __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, l * 16, t < turns ? first + block * 4096 + t * step : 0x7fffffff, 2));
+    return __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, t < turns ? l * 16 : INT32_MIN, t < turns ? first + block * 4096 + t * step : 0, 2));
   };
   i32x4 cur[FEW_AHEAD];
 #pragma unroll
@@ -349,7 +349,7 @@ __global__ __launch_bounds__(512) void gemm_int8_few_kernel(const bf16_t *__rest
     __syncthreads();
   }
 
-  const int8_t *mine = codes + min(l & 31, M - 1) * pitch + (wave >> 2) * 128 + (l >> 5) * 64 + (wave & 3) * 16;
+  [[maybe_unused]] const int8_t *mine = codes + min(l & 31, M - 1) * pitch + (wave >> 2) * 128 + (l >> 5) * 64 + (wave & 3) * 16;
   for (int block = blockIdx.x; block < blocks; block += gridDim.x) {
     i32x16 sum;
 #pragma unroll
