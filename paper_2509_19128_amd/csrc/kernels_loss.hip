@@ -71,8 +71,8 @@ struct Cut {
     c.nm = (count + 255) / 256;
     const int tiles = (vocab + TILE_V - 1) / TILE_V, fit = most / (c.nm > 0 ? c.nm : 1), far = (1 << 22) / (int)ldw;   // (W's rows of a piece lie behind one 32-bit offset)
     int p = fit < far ? fit : far;
-    if (p < 1) p = 1;
     if (c.nm > 0 && c.nm * p >= UNITS) p = c.nm * p / UNITS * UNITS / c.nm;
+    if (p < 1) p = 1;
     c.piece = p < tiles ? p : tiles;
     const int s = slices_most(c.nm, d);
     c.slice = (c.piece + s - 1) / s;

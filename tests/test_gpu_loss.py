@@ -22,6 +22,8 @@ def _stream():
 
 def _dev(a, pad=0, fill=float("nan")):
     """bf16 rows pad elements further apart than they are long (what lies between is NaN)."""
+    if isinstance(a, torch.Tensor):
+        return a
     t = torch.full((a.shape[0], a.shape[1] + pad), fill, dtype=torch.bfloat16)
     t[:, :a.shape[1]] = torch.from_numpy(np.ascontiguousarray(a))
     return t.cuda()
@@ -33,7 +35,7 @@ class Call:
     def __init__(self, h, w, target, it=None, pad=0):
         self.n, self.d, self.vocab, self.ld = len(h), h.shape[1], len(w), h.shape[1] + pad
         self.h, self.w = _dev(h, pad), _dev(w, pad)
-        self.target = torch.from_numpy(np.asarray(target, np.int32)).cuda()
+        self.target = target if isinstance(target, torch.Tensor) else torch.from_numpy(np.asarray(target, np.int32)).cuda()
         self.it = None if it is None else torch.from_numpy(np.asarray(it, np.float32)).cuda()
         self.args = (self.h.data_ptr(), self.ld, self.w.data_ptr(), self.ld, self.target.data_ptr(), 0 if it is None else self.it.data_ptr())
         self.shape = (self.n, self.vocab, self.d)
@@ -224,6 +226,94 @@ def test_rows_far_apart(n, ldh, ldw):
     lse = c.lse[:n].clone()
     c.backward(lse, torch.from_numpy(g).cuda())
     _check_gradients(c, h, w, target, lse.cpu().numpy().astype(np.float64), g.astype(np.float64), it)
+
+
+def _large(n, vocab, d, some, seed):
+    """A batch made on the device, `some` of whose positions have a target, half of those the last entry of the vocabulary."""
+    gen = torch.Generator("cuda").manual_seed(seed)
+    h = torch.randn((n, d), generator=gen, device="cuda", dtype=torch.bfloat16)
+    w = torch.randn((vocab, d), generator=gen, device="cuda", dtype=torch.bfloat16) * (1.2 / d ** 0.5)
+    target = torch.randint(0, vocab, (n,), generator=gen, device="cuda", dtype=torch.int32)
+    u = torch.rand(n, generator=gen, device="cuda")
+    target[u < some / 2] = vocab - 1
+    target[u > some] = -1
+    target[-1] = vocab - 1
+    return Call(h, w, target), torch.randn(n, generator=gen, device="cuda")
+
+
+def _check_large(c, g=None):
+    """_check_forward and _check_gradients on the device, entries of the vocabulary some thousands at a time."""
+    torch.cuda.synchronize()
+    c.guards()
+    has = c.target >= 0
+    y, lse, logprob = c.target[has].long(), c.lse[:c.n][has].double(), c.logprob[:c.n][has].double()
+    assert (c.lse[:c.n][~has] == 0).all() and (c.logprob[:c.n][~has] == 0).all()
+    h = c.h[has].double()
+    step = max(1, (1 << 28) // len(h) // 256 * 256)
+    sum_z, most, of_target, e_z = torch.zeros_like(lse), torch.full_like(lse, -float("inf")), torch.zeros_like(lse), torch.zeros_like(lse)
+    if g is not None:
+        g = g[has].double()[:, None]
+        dh, e_dh, G_w = (torch.zeros_like(h) for _ in range(3))
+        got_w = c.dw[:c.vocab * c.d].reshape(c.vocab, c.d)
+
+    def close(got, ref, e):
+        off = (got.double() - ref).abs() - (e + 2.0 ** -8 * (ref.abs() + e) + 1e-38)
+        assert off.max().item() <= 0, off.max().item()
+    for v in range(0, c.vocab, step):
+        w = c.w[v:v + step].double()
+        z, e = h @ w.T, (c.d + 2) * 2.0 ** -24 * (h.abs() @ w.abs().T)
+        top = torch.maximum(most, z.max(1).values)
+        sum_z = sum_z * (most - top).exp() + (z - top[:, None]).exp().sum(1)
+        most, e_z = top, torch.maximum(e_z, e.max(1).values)
+        hot = torch.arange(v, v + len(w), device="cuda")[None] == y[:, None]
+        of_target += torch.where(hot, z, torch.zeros_like(z)).sum(1)
+        if g is not None:
+            p = (z - lse[:, None]).exp()
+            G = g * (hot.double() - p)
+            e_G = g.abs() * p * (e + 2.0 ** -20 + 2.0 ** -23 * lse.abs()[:, None]) + 2.0 ** -22 * g.abs() * (hot + p) + 2.0 ** -8 * G.abs()
+            dh += G @ w
+            e_dh += e_G @ w.abs()
+            G_w += G.abs() @ w.abs()
+            close(got_w[v:v + step], G.T @ h, e_G.T @ h.abs() + (len(h) + 64) * 2.0 ** -24 * (G.abs().T @ h.abs()))
+    ref = most + sum_z.log()
+    e_lse = e_z + 2.0 ** -19 + 2.0 ** -23 * ref.abs()
+    assert ((lse - ref).abs() <= e_lse).all()
+    assert ((logprob - (of_target - ref)).abs() <= e_lse + e_z + 2.0 ** -23 * (of_target - ref).abs()).all()
+    if g is not None:
+        got_h = c.dh[:c.n * c.d].reshape(c.n, c.d)
+        assert (got_h[~has] == 0).all()
+        close(got_h[has], dh, e_dh + (c.vocab + 64) * 2.0 ** -24 * G_w)
+
+
+@pytest.mark.parametrize("n,vocab,d,some", [(400001, 600, 256, 1.0), (400001, 300, 256, 0.5), (1000, 500, 65536, 0.9), (16, 1000, 65536, 1.0), (3, 1 << 24, 256, 1.0),
+                                            (2000, 300000, 256, 0.7)])
+def test_large_batches_and_gradients(n, vocab, d, some):
+    c, g = _large(n, vocab, d, some, n + vocab)
+    c.forward()
+    c.backward(c.lse[:n].clone(), g)
+    _check_large(c, g)
+
+
+def test_the_most_positions():
+    n = 1 << 24
+    gen = torch.Generator("cuda").manual_seed(1)
+    h = torch.randn((n, 256), generator=gen, device="cuda", dtype=torch.bfloat16)
+    w = torch.randn((40, 256), generator=gen, device="cuda", dtype=torch.bfloat16) * 0.1
+    target = torch.randint(-3000, 40, (n,), generator=gen, device="cuda", dtype=torch.int32).clamp_(min=-1)
+    target[-1] = 39
+    logprob, lse = (torch.full((n + GUARD,), -7.0, device="cuda") for _ in range(2))
+    ws = torch.empty(pl.pl_token_logprob_workspace_bytes(n, 40, 256), dtype=torch.uint8, device="cuda")
+    pl.pl_token_logprob(h.data_ptr(), 256, w.data_ptr(), 256, target.data_ptr(), 0, logprob.data_ptr(), lse.data_ptr(), n, 40, 256, ws.data_ptr(), _stream())
+    torch.cuda.synchronize()
+    has = target >= 0
+    z = h[has].double() @ w.double().T
+    e_z = 258 * 2.0 ** -24 * (h[has].double().abs() @ w.double().abs().T).max(1).values
+    ref = z.logsumexp(1)
+    e_lse = e_z + 2.0 ** -19 + 2.0 ** -23 * ref.abs()
+    ref_lp = z.gather(1, target[has].long()[:, None])[:, 0] - ref
+    assert ((lse[:n][has] - ref).abs() <= e_lse).all()
+    assert ((logprob[:n][has] - ref_lp).abs() <= e_lse + e_z + 2.0 ** -23 * ref_lp.abs()).all()
+    assert (lse[:n][~has] == 0).all() and (logprob[:n][~has] == 0).all() and (lse[n:] == -7).all() and (logprob[n:] == -7).all()
 
 
 def test_temperatures_of_zero_and_below():
