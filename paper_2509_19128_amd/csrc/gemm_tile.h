@@ -128,7 +128,7 @@ struct Tile {
   __device__ __forceinline__ void rows_w(const bf16_t *W, int bytes) { rw = __builtin_amdgcn_make_buffer_rsrc((void *)W, 0, bytes, 0x00020000); }
   __device__ __forceinline__ void row_w(int b, int at) { w_lane[b] = at < 0 ? 0x7fff0000 : at * 2 + half * 64; }
   // (What lies beyond an operand reads as 0 by the check of its resource's size, which takes lane and scalar offset together, a scalar offset beyond the
-  // size too: measured for sizes from 0 to 2 GiB, into registers and into LDS.)
+  // size too: measured for sizes from 0 to 3 GiB, offsets up to 4, into registers and into LDS.)
   // x: rows (TILE_COLS_T: k) ldx elements apart from X on, of which `rows` exist (further ones read as 0); TILE_ROWS_T: an image of ldx rows, from the plane at
   // X on, of which `rows` planes of 64 exist;
   // w: operand-ordered, `n` of its rows per plane and `planes` k-steps from W on (further ones read as 0), the tile's from w_row on.
@@ -137,7 +137,7 @@ struct Tile {
     w_plane = (uint32_t)(n >> 5) * 4096u;
     if (!W_ROWS) rw = __builtin_amdgcn_make_buffer_rsrc((void *)W, 0, (int)((uint32_t)planes * w_plane), 0x00020000);
     const int64_t x_bytes = (int64_t)rows * ldx * (KIND == TILE_ROWS_T ? 128 : 2);
-    rx = __builtin_amdgcn_make_buffer_rsrc((void *)X, 0, (int)min(x_bytes, (int64_t)0x7fffffff), 0x00020000);
+    rx = __builtin_amdgcn_make_buffer_rsrc((void *)X, 0, (int)(uint32_t)min(x_bytes, (int64_t)1 << 31), 0x00020000);
     constexpr int PER = KIND == TILE_COLS_T ? BM / 8 : BK / 8, ROWS = 64 / PER;   // chunks of a row (of 64 k or of BM columns), rows of a load
     static_assert(KIND != TILE_COLS_T || ROWS * XL == 4, "the slots of a row go by its number modulo 4");
     static_assert(KIND != TILE_ROWS_T || XI == 8, "a wavefront loads a plane's part of a k-step");

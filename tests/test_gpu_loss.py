@@ -286,7 +286,7 @@ def _check_large(c, g=None):
 
 
 @pytest.mark.parametrize("n,vocab,d,some", [(400001, 600, 256, 1.0), (400001, 300, 256, 0.5), (1000, 500, 65536, 0.9), (16, 1000, 65536, 1.0), (3, 1 << 24, 256, 1.0),
-                                            (2000, 300000, 256, 0.7)])
+                                            (2000, 300000, 256, 0.7), (1000, 65536, 16384, 1.0)])
 def test_large_batches_and_gradients(n, vocab, d, some):
     c, g = _large(n, vocab, d, some, n + vocab)
     c.forward()
