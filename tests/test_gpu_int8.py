@@ -209,6 +209,29 @@ def test_replays_of_a_captured_product_with_eager_calls_between():
         _same(y2, ref[0])
 
 
+@pytest.mark.parametrize("N,K", [(512, 256), (3584, 3584)])
+def test_graphs_of_every_cut_share_a_workspace_at_an_odd_address(N, K):
+    rng = np.random.default_rng(14)
+    x, w = _inputs(rng, 600, N, K)
+    image, sw = quantize(w)
+    ref = int8.product(*int8.quantize_rows(x), *int8.quantize_rows(w))
+    xd = _dev(x, torch.bfloat16)
+    ws = torch.empty(pl.pl_gemm_int8_workspace_bytes(600, N, K) + 3 + max(pl.pl_gemm_int8_workspace_bytes(m, N, K) for m in (2, 24, 200)), dtype=torch.uint8, device="cuda")
+    calls = []
+    for M in (2, 24, 200, 600):
+        y, graph = torch.empty(M, N, device="cuda", dtype=torch.bfloat16), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            pl.pl_gemm_int8(xd.data_ptr(), K, image.data_ptr(), sw.data_ptr(), y.data_ptr(), pl.PL_BF16, M, N, K, ws.data_ptr() + 3, torch.cuda.current_stream().cuda_stream)
+        calls.append((M, y, graph))
+    for _ in range(3):
+        for M, y, graph in calls:
+            ws.fill_(255)
+            y.fill_(-1)
+            graph.replay()
+            torch.cuda.synchronize()
+            _same(y, ref[:M])
+
+
 def test_two_streams_at_once_with_workspaces_of_their_own():
     rng = np.random.default_rng(13)
     M, N, K = 40, 2048, 2048

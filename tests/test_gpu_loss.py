@@ -432,6 +432,69 @@ def test_results_are_the_same_bits_from_call_to_call_and_replay_from_a_graph():
             assert np.array_equal(a, b)
 
 
+@pytest.mark.parametrize("n,vocab", [(20, 700), (100, 700), (1500, 150000)])
+def test_replays_find_other_targets_and_two_graphs_share_workspaces(n, vocab):
+    """Which positions have a target is found out as a replay runs; 1500 positions of 150000 entries take several pieces.  Graphs replayed in turn leave nothing
+    in workspaces, at odd addresses here, that the other one would read."""
+    d = 256
+    batches = []
+    calls = [_large(n, vocab, d, 0.9, 5 + i) for i in range(2)]
+    lse = [torch.empty(n, device="cuda") for _ in calls]
+    raw = [torch.empty(b + 3, dtype=torch.uint8, device="cuda") for b in calls[0][0].sizes]
+
+    def both(i):
+        c, g = calls[i]
+        pl.pl_token_logprob(*c.args, c.logprob.data_ptr(), c.lse.data_ptr(), *c.shape, raw[0].data_ptr() + 3, _stream())
+        lse[i].copy_(c.lse[:n])
+        pl.pl_token_logprob_grad(*c.args, lse[i].data_ptr(), g.data_ptr(), c.dh.data_ptr(), c.dw.data_ptr(), *c.shape, raw[1].data_ptr() + 3, _stream())
+
+    gen = torch.Generator("cuda").manual_seed(9)
+    for some in (1.0, 0.05, 0.0, 0.6):
+        t = torch.randint(0, vocab, (n,), generator=gen, device="cuda", dtype=torch.int32)
+        t[torch.rand(n, generator=gen, device="cuda") >= some] = -1
+        batches.append(t)
+    ref = {}
+    for i, (c, _) in enumerate(calls):
+        for k, t in enumerate(batches):
+            c.target.copy_(t)
+            both(i)
+            ref[i, k] = [x.clone() for x in (c.logprob, c.lse, c.dh, c.dw)]
+            if k in (0, 3) and vocab < 1000:
+                _check_large(*calls[i])
+    graphs = [torch.cuda.CUDAGraph() for _ in calls]
+    for i, graph in enumerate(graphs):
+        with torch.cuda.graph(graph):
+            both(i)
+    for k in (0, 2, 1, 3, 0, 3):
+        for i, (c, _) in enumerate(calls):
+            c.target.copy_(batches[k])
+            for x in (c.logprob[:n], c.lse[:n], c.dh[:n * d], c.dw[:vocab * d]):
+                x.fill_(3)
+            for w_s in raw:
+                w_s.fill_(255)
+            graphs[i].replay()
+            for a, b in zip((c.logprob, c.lse, c.dh, c.dw), ref[i, k]):
+                assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("n", [20, 90, 300])
+def test_a_bad_position_leaves_the_other_rows_of_dh(n):
+    h, w, target, it, rng = _batch(n, 900, 512, 90 + n)
+    c = Call(h, w, target, it)
+    c.forward()
+    g = torch.from_numpy(rng.normal(size=n).astype(np.float32)).cuda()
+    lse = c.lse[:n].clone()
+    target[3] = c.target[3] = 5
+    c.backward(lse, g, dw=False)
+    want = c.gradients()[0]
+    g[3] = float("nan")
+    c.h[3] = float("inf")
+    c.backward(lse, g, dw=False)
+    got = c.gradients()[0]
+    others = np.arange(n) != 3
+    assert np.array_equal(got[others], want[others]) and np.isnan(got[3]).all()
+
+
 def test_two_streams_at_once():
     calls = []
     for i in range(2):
