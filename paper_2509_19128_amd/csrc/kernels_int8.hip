@@ -5,7 +5,7 @@
 // in int32 without error (127^2 K < 2^31), in any order and any number of slices, and a result is (float(sum) * scale of its token) * scale of
 // its channel.
 //
-// The product is gemm_tile.h's: W's codes in operand order straight to the registers of the first operand, x's through LDS.  Bytes per k-step and cycles
+// The product is gemm_tile.h's, but for few rows (gemm_int8_few_kernel, gemm_int8_narrow_kernel): W's codes in operand order straight to the registers of the first operand, x's through LDS.  Bytes per k-step and cycles
 // of a matrix instruction are those of the bf16 product at twice the k, so a byte of weights does twice the work in both bounds.
 #include "gemm_tile.h"
 
@@ -134,10 +134,12 @@ __global__ __launch_bounds__(1024) void quantize_weights_kernel(const T *__restr
   }
 }
 
-// Codes of x, row-major, rows padded with zeros to k_pad.  A workgroup per row, eight values of a lane at a time.
-__global__ __launch_bounds__(1024) void quantize_rows_kernel(const bf16_t *__restrict__ x, int64_t ldx, uint2 *__restrict__ q, float *__restrict__ scale, int K, int k_pad) {
+// Codes of x, row-major, rows padded with zeros to k_pad, or (ORDERED) in operand order, `blocks` blocks of 32 rows.  A workgroup per row, eight values of a
+// lane at a time.
+template <bool ORDERED>
+__global__ __launch_bounds__(1024) void quantize_rows_kernel(const bf16_t *__restrict__ x, int64_t ldx, uint2 *__restrict__ q, float *__restrict__ scale, int K, int k_pad, int blocks) {
   x += blockIdx.x * ldx;
-  q += (int64_t)blockIdx.x * (k_pad >> 3);
+  q += ORDERED ? (int64_t)(blockIdx.x >> 5) * 512 + (blockIdx.x & 31) * 2 : (int64_t)blockIdx.x * (k_pad >> 3);
   const int pieces = K >> 3;
   Values<bf16_t, 8> v;
   float m = 0.f;
@@ -156,7 +158,8 @@ __global__ __launch_bounds__(1024) void quantize_rows_kernel(const bf16_t *__res
     if (p < pieces && pieces > (int)blockDim.x) v.load(x + p * 8);   // (otherwise the one piece is still here)
     uint32_t c[2] = {0, 0};
     if (p < pieces) v.codes(rs, c);
-    q[p] = make_uint2(c[0], c[1]);
+    // (in order: eight codes of block p / 16, quarter p / 2 % 4, half p / 8 % 2)
+    q[ORDERED ? (int64_t)(p >> 4) * blocks * 512 + ((p >> 1) & 3) * 128 + ((p >> 3) & 1) * 64 + (p & 1) : p] = make_uint2(c[0], c[1]);
   }
 }
 
@@ -382,6 +385,59 @@ __global__ __launch_bounds__(512) void gemm_int8_few_kernel(const bf16_t *__rest
   }
 }
 
+// Narrow outputs of few rows: a workgroup takes 16 channels over all of K, its eight wavefronts turns of 64 k (1 KiB of W, in four pieces) with the same k of
+// x's codes, in operand order too, straight from memory; at the end their sums are added up in LDS.  No slices that a launch behind would add up.
+// BLOCKS: of 16 rows.
+template <int BLOCKS, bool COLD, typename T>
+__global__ __launch_bounds__(512) void gemm_int8_narrow_kernel(const int8_t *__restrict__ xq, const int8_t *__restrict__ wq, const float *__restrict__ sx, const float *__restrict__ sw,
+                                                               T *__restrict__ y, int M, int N, int K) {
+  constexpr int AHEAD = BLOCKS > 1 ? 2 : 4, PAIRS = (BLOCKS + 1) / 2;   // (turns in flight per wavefront; 8: 1536 x 1536, 8 rows, 5.7 -> 6.6 us)
+  __shared__ i32x4 sums[8][BLOCKS][64];
+  const int l = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), planes = K >> 7, n0 = blockIdx.x * 16;
+  const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc((void *)wq, 0, (int)((int64_t)N * K), 0x00020000);
+  const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc((void *)xq, 0, PAIRS * 32 * K, 0x00020000);
+  // a lane's sixteen k: quarter l / 16 of the half that its wavefront has of a plane of 128 (both operands' alike, so that which k these are is no matter)
+  const int lane = (l >> 4) * 1024 + (l & 15) * 16, w_first = (n0 >> 5) * 4096 + (wave & 1) * 512 + ((n0 >> 4) & 1) * 256;
+  i32x4 w[AHEAD], x[AHEAD][BLOCKS], sum[BLOCKS];
+  auto load = [&](int u, int t) {   // (planes behind K: zeros, from 2 GiB on)
+    const int plane = t * 4 + (wave >> 1), at = plane < planes ? lane : INT32_MIN;
+    w[u] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, at, plane < planes ? w_first + plane * N * 128 : 0, COLD ? 2 : 0));
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b)
+      x[u][b] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rx, at, plane < planes ? (plane * PAIRS + b / 2) * 4096 + (wave & 1) * 512 + (b & 1) * 256 : 0, 0));
+  };
+#pragma unroll
+  for (int u = 0; u < AHEAD; ++u) load(u, u);
+#pragma unroll
+  for (int b = 0; b < BLOCKS; ++b) sum[b] = i32x4{0, 0, 0, 0};
+  for (int t = 0; t * 4 < planes; t += AHEAD)
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+#ifdef __HIP_DEVICE_COMPILE__
+#pragma unroll
+      for (int b = 0; b < BLOCKS; ++b) sum[b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[u], x[u][b], sum[b], 0, 0, 0);
+#endif
+      load(u, t + u + AHEAD);
+    }
+  // register i of lane l: channel l / 16 * 4 + i, row l % 16
+#pragma unroll
+  for (int b = 0; b < BLOCKS; ++b) sums[wave][b][l] = sum[b];
+  __syncthreads();
+  if (wave >= BLOCKS) return;
+  i32x4 s = {0, 0, 0, 0};
+#pragma unroll
+  for (int k = 0; k < 8; ++k) s += sums[k][wave][l];
+  const int m = wave * 16 + (l & 15), n = n0 + (l >> 4) * 4;
+  if (m >= M) return;
+  const float a = sx[m];
+  f32x4 r;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) r[e] = (float)s[e] * a * sw[n + e];
+  T *to = y + (int64_t)m * N + n;
+  if constexpr (sizeof(T) == 4) *(f32x4 *)to = r;
+  else *(uint2 *)to = make_uint2(two_bf16(r[0], r[1]), two_bf16(r[2], r[3]));
+}
+
 int done() { return hipGetLastError() == hipSuccess ? 0 : -7; }
 int64_t align256(int64_t b) { return (b + 255) / 256 * 256; }
 
@@ -389,7 +445,7 @@ int64_t align256(int64_t b) { return (b + 255) / 256 * 256; }
 // more * (average beyond one workgroup per unit) + round * (workgroups of the fullest unit - 1)), out per MB of bf16 results, and with slices their
 // launch and MB of sums.  Fitted to 2700 launches (the products of the 1.5B, 7B and 32B shapes and smaller ones, 1 to 3001 rows, 1 to 24 slices, weights
 // not in the last-level cache): the choice takes 1.2 % more than the best measured one on average, 6 % in 95 of 100.
-enum { I8_32x128, I8_64x128, I8_128x128, I8_128x256, I8_64x64, I8_ROUNDS, I8_FEW };
+enum { I8_32x128, I8_64x128, I8_128x128, I8_128x256, I8_64x64, I8_ROUNDS, I8_FEW, I8_NARROW };
 struct ShapeTime { int rows, cols; float fixed, base, load, more, round, slices, slice_mb, out_mb; };
 constexpr ShapeTime SHAPES[] = {{32, 128, 5.29f, 0.275f, 0.137f, 0.128f, 0.217f, 4.46f, 0.203f, 0.f},   {64, 128, 5.88f, 0.324f, 0.197f, 0.155f, 0.25f, 3.67f, 0.371f, 0.f},
                                 {128, 128, 7.75f, 0.359f, 0.289f, 0.278f, 0.313f, 2.88f, 0.386f, 0.098f}, {128, 256, 8.39f, 0.625f, 0.623f, 0.419f, 0.707f, 2.75f, 0.337f, 0.067f},
@@ -403,6 +459,14 @@ bool few_fits(int M, int K) { return M <= 4 && few_rows(M) * K <= 512 * FEW_HELD
 float few_us(int M, int N, int K) {
   const float rounds = (N / 32 + 2 * UNITS - 1) / (2 * UNITS);
   return std::max(2.8f + 1.5e-4f * few_rows(M) * K + rounds * K * (32 / 45e3f), 1.f + (float)N * K * (1 / 6.4e6f));
+}
+// gemm_int8_narrow_kernel, a workgroup per unit at most.  us on the device, with slices or 64 x 64 tiles / so, weights from memory: 8 rows 1536 x 3584 10.6 / 7.5,
+// 4096 x 3584 12.2 / 8.6, 4096 x 7168 14.8 / 12.1; 64 rows 2560 x 2560 11.6 / 9.5, 4096 x 5120 15.4 / 13.6, 2560 x 7168 16.1 / 16.3; in the cache: 8 rows
+// 1536 x 8960 10.0 / 11.0, 4608 x 3584 (two on a unit) 9.8 / 9.9, 19 rows 10.4 / 11.4.
+int row_blocks(int M) { return (M + 31) / 32; }
+float narrow_us(int M, int N, int K) {
+  if (M > 64 || N > 16 * UNITS) return 1e30f;
+  return 3.7f + K * (0.5e-3f + 0.25e-3f * ((M + 15) / 16)) + 5e-8f * N * K;
 }
 Int8Plan int8_plan(int M, int N, int K) {
   const int groups = (K + K_UNIT - 1) / K_UNIT;
@@ -429,6 +493,7 @@ Int8Plan int8_plan(int M, int N, int K) {
     }
   }
   if (few < best_us) best = Int8Plan{I8_FEW, 1, 0};
+  if (narrow_us(M, N, K) < std::min(few, best_us)) best = Int8Plan{I8_NARROW, 1, 0};
   return best;
 }
 
@@ -464,7 +529,8 @@ int launch_quantize_int8(const void *w, bool f32, int64_t ldw, int8_t *q, float 
 
 int64_t gemm_int8_workspace_bytes(int M, int N, int K) {
   const Int8Plan p = int8_plan(M, N, K);
-  return align256((int64_t)M * 4) + align256((int64_t)M * ((K + K_UNIT - 1) / K_UNIT * K_UNIT)) + (p.splits > 1 ? (int64_t)p.splits * M * N * 4 : 0);
+  const int64_t codes = p.shape == I8_NARROW ? (int64_t)row_blocks(M) * 32 * K : (int64_t)M * ((K + K_UNIT - 1) / K_UNIT * K_UNIT);
+  return align256((int64_t)M * 4) + align256(codes) + (p.splits > 1 ? (int64_t)p.splits * M * N * 4 : 0);
 }
 
 int launch_gemm_int8(const bf16_t *x, int64_t ldx, const int8_t *wq, const float *sw, void *y, bool f32, int M, int N, int K, void *ws, hipStream_t s) {
@@ -483,11 +549,32 @@ int launch_gemm_int8(const bf16_t *x, int64_t ldx, const int8_t *wq, const float
     if (f32) with((float *)y); else with((bf16_t *)y);
     return done();
   }
-  const int k_pad = (K + K_UNIT - 1) / K_UNIT * K_UNIT;
+  const int k_pad = plan.shape == I8_NARROW ? K : (K + K_UNIT - 1) / K_UNIT * K_UNIT;
   float *sx = (float *)ws;
   int8_t *xq = (int8_t *)ws + align256((int64_t)M * 4);
+  auto quantize = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3(M), dim3(std::min(1024, (K / 8 + 63) / 64 * 64)), 0, s, x, ldx, (uint2 *)xq, sx, K, k_pad, row_blocks(M));
+  };
+  if (plan.shape == I8_NARROW) {
+    quantize(quantize_rows_kernel<true>);
+    auto launch = [&](auto kernel, auto *out) { hipLaunchKernelGGL(kernel, dim3(N / 16), dim3(512), 0, s, xq, wq, sx, sw, out, M, N, K); };
+    auto with = [&](auto *out, auto COLD) {
+      typedef std::remove_pointer_t<decltype(out)> T;
+      switch ((M + 15) / 16) {
+        case 1: launch(gemm_int8_narrow_kernel<1, COLD.value, T>, out); break;
+        case 2: launch(gemm_int8_narrow_kernel<2, COLD.value, T>, out); break;
+        case 3: launch(gemm_int8_narrow_kernel<3, COLD.value, T>, out); break;
+        default: launch(gemm_int8_narrow_kernel<4, COLD.value, T>, out);
+      }
+    };
+    auto cold = [&](auto *out) {
+      if ((int64_t)N * K > (8 << 20)) with(out, std::true_type{}); else with(out, std::false_type{});
+    };
+    if (f32) cold((float *)y); else cold((bf16_t *)y);
+    return done();
+  }
+  quantize(quantize_rows_kernel<false>);
   int32_t *slices = (int32_t *)(xq + align256((int64_t)M * k_pad));
-  hipLaunchKernelGGL(quantize_rows_kernel, dim3(M), dim3(std::min(1024, (K / 8 + 63) / 64 * 64)), 0, s, x, ldx, (uint2 *)xq, sx, K, k_pad);
   Int8Params g{xq, wq, sx, sw, plan.splits > 1 ? (void *)slices : y, M, N, K, k_pad, plan.splits, plan.slice,
                (N + SHAPES[plan.shape].cols - 1) / SHAPES[plan.shape].cols, (M + SHAPES[plan.shape].rows - 1) / SHAPES[plan.shape].rows};
   const int out = plan.splits > 1 ? OUT_SLICES : f32 ? OUT_F32 : OUT_BF16;

@@ -172,6 +172,18 @@ def test_few_rows_and_bad_ones_among_them(M, N, K):
         _same(product(_bf16(x), torch.from_numpy(int8.operand_image(wq)).cuda(), scales[1:], N, out), int8.product(*int8.quantize_rows(_bf16(x)), wq, sw))
 
 
+@pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("M", [5, 16, 17, 33, 49, 64])
+@pytest.mark.parametrize("N,K", [(4096, 2560), (4096, 6912), (4128, 2560)])
+def test_narrow_outputs_of_large_weights(M, N, K, out):
+    rng = np.random.default_rng(M + N + K)
+    x, w = _inputs(rng, M, N, K)
+    x[M // 2, 3] = np.nan
+    wq, sw = int8.quantize_rows(w)
+    scales = torch.from_numpy(sw).cuda()
+    _same(product(_bf16(x), torch.from_numpy(int8.operand_image(wq)).cuda(), scales, N, out, pad=8), int8.product(*int8.quantize_rows(_bf16(x)), wq, sw))
+
+
 def test_millions_of_channels():
     """One row against a W whose turns behind K would lie beyond 32 bits: equal to the same row in a call of five, which takes other kernels."""
     N, K = 2560000, 256
