@@ -55,10 +55,6 @@ struct RowScale {
            (uint32_t)quotient(x3 * up, s, inv) << 24;
   }
 };
-__device__ inline float magnitude(float x, float m) {   // infinity stands for NaN too
-  const float a = fabsf(x);
-  return a < INFINITY ? fmaxf(m, a) : INFINITY;
-}
 // COUNT consecutive values of a row
 template <typename T, int COUNT>
 struct Values {
@@ -76,10 +72,26 @@ struct Values {
     if constexpr (sizeof(T) == 4) return __uint_as_float(d);
     else return __uint_as_float(i & 1 ? d & 0xffff0000u : d << 16);
   }
-  __device__ __forceinline__ float most(float m) const {
+  // The largest magnitude as an unsigned number, which orders bit patterns without sign as their values are, infinities and NaN last: one or two
+  // instructions a value.  (bf16: two side by side.)
+  struct Most {
+    typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
+    std::conditional_t<sizeof(T) == 4, uint32_t, u16x2> m{};
+    __device__ __forceinline__ float value() const {   // infinity stands for NaN too
+      uint32_t bits;
+      if constexpr (sizeof(T) == 4) bits = m;
+      else bits = (uint32_t)max(m[0], m[1]) << 16;
+      return bits < 0x7f800000u ? __uint_as_float(bits) : INFINITY;
+    }
+  };
+  __device__ __forceinline__ void most(Most &m) const {
 #pragma unroll
-    for (int i = 0; i < COUNT; ++i) m = magnitude(get(i), m);
-    return m;
+    for (int i = 0; i < VECTORS * 4; ++i) {
+      const uint4 u = raw[i / 4];
+      const uint32_t d = i % 4 == 0 ? u.x : i % 4 == 1 ? u.y : i % 4 == 2 ? u.z : u.w;
+      if constexpr (sizeof(T) == 4) m.m = max(m.m, d & 0x7fffffffu);
+      else m.m = __builtin_elementwise_max(m.m, __builtin_bit_cast(typename Most::u16x2, d & 0x7fff7fffu));
+    }
   }
   __device__ __forceinline__ void codes(const RowScale &r, uint32_t (&q)[COUNT / 4]) const {
 #pragma unroll
@@ -94,21 +106,22 @@ __global__ __launch_bounds__(1024) void quantize_weights_kernel(const T *__restr
   const int r = threadIdx.x & 7, row = blockIdx.x * 8 + r, lanes = blockDim.x >> 3, first = threadIdx.x >> 3, pieces = K >> 4;
   w += row * ldw;
   Values<T, 16> held[HELD ? HELD : 1];
-  float m = 0.f;
+  typename Values<T, 16>::Most most;
   if constexpr (HELD > 0) {
 #pragma unroll
     for (int u = 0; u < HELD; ++u)
       if (first + u * lanes < pieces) held[u].load(w + (first + u * lanes) * 16);
 #pragma unroll
     for (int u = 0; u < HELD; ++u)
-      if (first + u * lanes < pieces) m = held[u].most(m);
+      if (first + u * lanes < pieces) held[u].most(most);
   } else {
     for (int p = first; p < pieces; p += lanes) {
       held[0].load(w + p * 16);
-      m = held[0].most(m);
+      held[0].most(most);
     }
   }
   __shared__ float part[16][8];
+  float m = most.value();
   m = fmaxf(m, dpp<DPP_ROR8>(m));
   m = with_xor16(m, OpMax{});
   m = with_xor32(m, OpMax{});
@@ -142,13 +155,13 @@ __global__ __launch_bounds__(1024) void quantize_rows_kernel(const bf16_t *__res
   q += ORDERED ? (int64_t)(blockIdx.x >> 5) * 512 + (blockIdx.x & 31) * 2 : (int64_t)blockIdx.x * (k_pad >> 3);
   const int pieces = K >> 3;
   Values<bf16_t, 8> v;
-  float m = 0.f;
+  Values<bf16_t, 8>::Most most;
   for (int p = threadIdx.x; p < pieces; p += blockDim.x) {
     v.load(x + p * 8);
-    m = v.most(m);
+    v.most(most);
   }
   __shared__ float part[16];
-  m = wave_max(m);
+  float m = wave_max(most.value());
   if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
   __syncthreads();
   for (int i = 0; i < (int)blockDim.x >> 6; ++i) m = fmaxf(m, part[i]);
@@ -328,14 +341,14 @@ __global__ __launch_bounds__(512) void gemm_int8_few_kernel(const bf16_t *__rest
     const int row = wave / WAVES, at = threadIdx.x & (LANES - 1), pieces = K >> 3;   // (a row beyond M: the last one again, into no one's place)
     const bf16_t *mine = x + min(row, M - 1) * ldx;
     Values<bf16_t, 8> v[FEW_HELD];
-    float m = 0.f;
+    Values<bf16_t, 8>::Most most;
 #pragma unroll
     for (int u = 0; u < FEW_HELD; ++u)
       if (at + u * LANES < pieces) v[u].load(mine + (at + u * LANES) * 8);
 #pragma unroll
     for (int u = 0; u < FEW_HELD; ++u)
-      if (at + u * LANES < pieces) m = v[u].most(m);
-    m = wave_max(m);
+      if (at + u * LANES < pieces) v[u].most(most);
+    float m = wave_max(most.value());
     if (l == 0) part[wave] = m;
     __syncthreads();
 #pragma unroll
