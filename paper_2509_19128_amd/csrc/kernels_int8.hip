@@ -14,6 +14,7 @@
 namespace pl {
 namespace {
 
+constexpr int DPP_ROR2 = 0x122;
 constexpr int K_UNIT = 512;   // codes of four k-steps: rows of x are padded with zeros to a multiple, W reads as zeros there
 constexpr int UNITS = 256;
 
@@ -99,11 +100,17 @@ struct Values {
   }
 };
 
-// Codes of weights in operand order.  Eight rows per workgroup: a 128-byte line of the image holds the same sixteen k of eight rows.  A lane keeps its
-// values between the two passes where they fit into HELD pieces of sixteen.
-template <typename T, int HELD>
+// Codes of weights in operand order.  ROWS rows per workgroup: a 128-byte line of the image holds the same sixteen k of eight rows, and workgroups that share
+// lines are on one XCD.  A lane keeps its values between the two passes where they fit into HELD pieces of sixteen.
+template <typename T, int HELD, int ROWS>
 __global__ __launch_bounds__(1024) void quantize_weights_kernel(const T *__restrict__ w, int64_t ldw, uint4 *__restrict__ q, float *__restrict__ scale, int N, int K) {
-  const int r = threadIdx.x & 7, row = blockIdx.x * 8 + r, lanes = blockDim.x >> 3, first = threadIdx.x >> 3, pieces = K >> 4;
+  const int r = threadIdx.x & (ROWS - 1), lanes = blockDim.x / ROWS, first = threadIdx.x / ROWS, pieces = K >> 4;
+  int block = blockIdx.x;
+  if constexpr (ROWS < 8) {   // (gridDim.x is a multiple of 8: N of 32)
+    const int each = gridDim.x >> 3;
+    block = (block & 7) * each + (block >> 3);
+  }
+  const int row = block * ROWS + r;
   w += row * ldw;
   Values<T, 16> held[HELD ? HELD : 1];
   typename Values<T, 16>::Most most;
@@ -120,12 +127,14 @@ __global__ __launch_bounds__(1024) void quantize_weights_kernel(const T *__restr
       held[0].most(most);
     }
   }
-  __shared__ float part[16][8];
+  __shared__ float part[16][ROWS];
   float m = most.value();
+  if constexpr (ROWS < 4) m = fmaxf(m, dpp<DPP_ROR2>(m));
+  if constexpr (ROWS < 8) m = fmaxf(m, dpp<DPP_ROR4>(m));
   m = fmaxf(m, dpp<DPP_ROR8>(m));
   m = with_xor16(m, OpMax{});
   m = with_xor32(m, OpMax{});
-  if ((threadIdx.x & 63) < 8) part[threadIdx.x >> 6][r] = m;
+  if ((threadIdx.x & 63) < ROWS) part[threadIdx.x >> 6][r] = m;
   __syncthreads();
   for (int i = 0; i < (int)blockDim.x >> 6; ++i) m = fmaxf(m, part[i][r]);
   const RowScale rs(m);
@@ -524,12 +533,23 @@ void launch_shape(const Int8Params &g, int out, bool cold, hipStream_t s) {
 
 template <typename T>
 void launch_weights(const T *w, int64_t ldw, int8_t *q, float *scale, int N, int K, hipStream_t s) {
-  // lanes of a row so that it takes at most HELD pieces of a lane: 32, 64 or 128 (more pieces would not fit a lane's 128 registers)
+  // Lanes of a row so that it takes at most HELD pieces of a lane (more would not fit a lane's 128 registers); the longest rows are read twice.
+  // us, with a product of eight rows behind, read twice by 128 lanes / held by 256 or 512: fp32 5120 x 27648 274 / 183, 1024 x 20480 54 / 32, bf16 5120 x
+  // 27648 152 / 131.  Rows of a workgroup: whole lines, but workgroups of 1024 threads are alone on a unit and overlap nothing (eight rows of 128 lanes /
+  // four: fp32 4128 x 8192 64 / 44, bf16 16384 x 8192 113 / 106), and few rows leave units without work (eight / two: bf16 512 x 1536 18.4 / 15.8;
+  // four / two: bf16 3584 x 18944 67 / 60, but 5120 x 27648 131 / 140).
   constexpr int HELD = sizeof(T) == 4 ? 5 : 7;
-  const int pieces = K / 16, lanes = pieces <= 32 * HELD ? 32 : pieces <= 64 * HELD ? 64 : 128;
-  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(N / 8), dim3(lanes * 8), 0, s, w, ldw, (uint4 *)q, scale, N, K); };
-  if (pieces <= lanes * HELD) launch(quantize_weights_kernel<T, HELD>);
-  else launch(quantize_weights_kernel<T, 0>);
+  const int pieces = K / 16;
+  int lanes = 32;
+  while (lanes < 512 && pieces > lanes * HELD) lanes *= 2;
+  auto launch = [&](auto ROWS) {
+    auto with = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(N / ROWS.value), dim3(lanes * ROWS.value), 0, s, w, ldw, (uint4 *)q, scale, N, K); };
+    if (pieces <= lanes * HELD) with(quantize_weights_kernel<T, HELD, ROWS.value>); else with(quantize_weights_kernel<T, 0, ROWS.value>);
+  };
+  const int rows = lanes <= 64 ? (N < 8 * UNITS ? 2 : 8) : lanes <= 256 && N >= 16 * UNITS ? 4 : 2;
+  if (rows == 8) launch(std::integral_constant<int, 8>{});
+  else if (rows == 4) launch(std::integral_constant<int, 4>{});
+  else launch(std::integral_constant<int, 2>{});
 }
 
 }  // namespace

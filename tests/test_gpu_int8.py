@@ -74,6 +74,20 @@ def test_codes_and_scales_of_weights(N, K, dtype, pad):
     assert np.array_equal(q.cpu().numpy(), int8.operand_image(ref_q))
 
 
+@pytest.mark.parametrize("dtype,pad", [("f32", 4), ("bf16", 0)])
+@pytest.mark.parametrize("N,K", [(4096, 256), (2048, 1792), (64, 8960), (4096, 7424), (32, 14592), (64, 28672), (4096, 20480), (32, 40960), (32, 41216), (96, 57344), (32, 57600)])
+def test_codes_of_every_row_length(N, K, dtype, pad):
+    rng = np.random.default_rng(N + K)
+    w = (rng.normal(size=(N, K)) * 0.02).astype(np.float32)
+    w[N // 2, K - 1], w[N - 1, 0], w[3] = 1.5, -np.inf, 0.0
+    if dtype == "bf16":
+        w = _bf16(w).astype(np.float32)
+    q, s = quantize(w, torch.float32 if dtype == "f32" else torch.bfloat16, pad)
+    ref_q, ref_s = int8.quantize_rows(w)
+    _same(s, ref_s)
+    assert np.array_equal(q.cpu().numpy(), int8.operand_image(ref_q).reshape(-1))
+
+
 def test_codes_of_hard_rows():
     """Ties (to even), the largest and smallest numbers, zeros, infinities and NaN."""
     rng = np.random.default_rng(3)
