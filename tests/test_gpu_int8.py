@@ -198,6 +198,15 @@ def test_narrow_outputs_of_large_weights(M, N, K, out):
     _same(product(_bf16(x), torch.from_numpy(int8.operand_image(wq)).cuda(), scales, N, out, pad=8), int8.product(*int8.quantize_rows(_bf16(x)), wq, sw))
 
 
+@pytest.mark.parametrize("M,K", [(5, 7936), (6, 8192), (70, 8448), (7, 32768), (130, 33024), (5, 33280), (9, 65536)])
+def test_rows_that_lanes_hold_and_longer_ones(M, K):
+    rng = np.random.default_rng(M + K)
+    x, w = _inputs(rng, M, 64, K)
+    x[1, K - 1], x[2, 0], x[3] = 300.0, np.inf, 0.0
+    wq, sw = int8.quantize_rows(w)
+    _same(product(_bf16(x), torch.from_numpy(int8.operand_image(wq)).cuda(), torch.from_numpy(sw).cuda(), 64, pad=16), int8.product(*int8.quantize_rows(_bf16(x)), wq, sw))
+
+
 def test_millions_of_channels():
     """One row against a W whose turns behind K would lie beyond 32 bits: equal to the same row in a call of five, which takes other kernels."""
     N, K = 2560000, 256
