@@ -405,7 +405,7 @@ int pl_is_ess(const float *logp_pi, const float *logp_mu, const int64_t *seq_off
  *   w       device bf16, vocab rows of d weights, ldw elements apart: row-major, as a trainer (and a tied embedding table) has them
  *   target  device int32 [n].  A value outside [0, vocab) means a position without a target (prompts, padding): its logprob and lse are
  *           0, and whatever its row of h holds (NaN included) reaches no other result.  Such positions cost nothing.
- *   inv_temperature  device fp32 [n], or NULL: 1.  A negative one (or NaN) gives its position NaN.
+ *   inv_temperature  device fp32 [n], or NULL: 1.  0 makes all tokens equally likely; a negative one, an infinity or NaN gives its position NaN.
  *   logprob, lse     device fp32 [n] out
  *   workspace        device, at least pl_token_logprob_workspace_bytes(n, vocab, d) bytes, nothing of value in it afterwards
  * bf16 products, fp32 sums.  A position's results do not depend on the other positions of the call, to the last bit.
@@ -423,7 +423,7 @@ int pl_token_logprob(const void *h, int64_t ldh, const void *w, int64_t ldw, con
  * lse and the first six arguments are those of the forward call (lse device fp32 [n], g device fp32 [n]; neither is read where there is no
  * target).  The logits are computed again, piece by piece of the vocabulary; G is rounded to bf16 for the products (half a step, as the
  * operands are; calls of up to 128 positions keep a second bf16 term of it), sums are fp32, results are rounded once.  Results are the same bits
- * from call to call.
+ * from call to call.  A NaN in g, lse or inv_temperature of a position with a target makes its row of dh NaN, and dw.
  * PL_E_INVAL as above, and for n * d * 2 bytes (n counted up to a multiple of 256) of 2 GiB or more, dh or dw not aligned to 16 bytes, neither asked for. */
 int64_t pl_token_logprob_grad_workspace_bytes(int32_t n, int32_t vocab, int32_t d);
 int pl_token_logprob_grad(const void *h, int64_t ldh, const void *w, int64_t ldw, const int32_t *target, const float *inv_temperature,

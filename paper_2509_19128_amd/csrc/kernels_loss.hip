@@ -29,7 +29,7 @@ constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 struct Row { float factor, lse2, scale; int32_t target; };
 // (not negative: the largest product has the largest logit; of 0 the smallest normal number, whose logits are 0 beside any sum of exponentials: entries beyond
 // the vocabulary, -inf, stay that and do not become 0 * inf)
-__device__ inline float logit_factor(float inv_t) { return inv_t >= 0.f ? fmaxf(inv_t * LOG2E, 0x1p-126f) : NAN; }
+__device__ inline float logit_factor(float inv_t) { return inv_t >= 0.f && inv_t < INFINITY ? fmaxf(inv_t * LOG2E, 0x1p-126f) : NAN; }
 
 // The workgroup numbers the positions with a target in order: each(position, has, number) for every position; returns how many there are.
 template <int THREADS, typename Each>

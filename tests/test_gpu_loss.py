@@ -329,6 +329,20 @@ def test_temperatures_of_zero_and_below():
     assert abs(lp[3] + np.log(vocab)) < 1e-5
 
 
+@pytest.mark.parametrize("n", [20, 100, 300])
+def test_infinite_temperatures_give_nan_and_leave_the_other_positions(n):
+    h, w, target, it, _ = _batch(n, 500, 256, 75 + n, masked=0.0)
+    it[7], it[n - 1] = np.inf, -np.inf
+    c = Call(h, -np.abs(w) if n == 100 else w, target, it)
+    c.forward()
+    bad = np.isin(np.arange(n), (7, n - 1))
+    for r in c.results():
+        assert np.isnan(r[bad]).all() and np.isfinite(r[~bad]).all()
+    c.backward(c.lse[:n].clone(), torch.ones(n, device="cuda"))
+    dh, dw = c.gradients()
+    assert np.isnan(dh[bad]).all() and np.isfinite(dh[~bad]).all() and np.isnan(dw).any()
+
+
 @pytest.mark.parametrize("n", [1, 30, 60, 100, 300])
 @pytest.mark.parametrize("vocab", [1, 500, 512])
 def test_inverse_temperatures_of_zero(n, vocab):
