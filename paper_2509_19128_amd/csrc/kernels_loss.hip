@@ -25,11 +25,11 @@ constexpr int PIECE = 8192;         // rows of a forward pass: 8 bytes per row a
 constexpr int UNITS = 256;          // workgroups of a kernel that walks tiles: one fills a compute unit
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
-// Logits are held in powers of two: z log2(e).  factor = inv_t log2(e), lse2 = lse log2(e), scale = g inv_t; padding: all 0, target -1
+// Exponentials are powers of two.  factor = inv_t log2(e), lse2 = lse log2(e), scale = g inv_t; padding: all 0, target -1
 struct Row { float factor, lse2, scale; int32_t target; };
 // (not negative: the largest product has the largest logit; of 0 the smallest normal number, whose logits are 0 beside any sum of exponentials: entries beyond
-// the vocabulary, -inf, stay that and do not become 0 * inf)
-__device__ inline float logit_factor(float inv_t) { return inv_t >= 0.f && inv_t < INFINITY ? fmaxf(inv_t * LOG2E, 0x1p-126f) : NAN; }
+// the vocabulary, -inf, stay that and do not become 0 * inf; finite, so that a difference of 0 stays one)
+__device__ inline float logit_factor(float inv_t) { return inv_t >= 0.f && inv_t < INFINITY ? fminf(fmaxf(inv_t * LOG2E, 0x1p-126f), 0x1.fffffep127f) : NAN; }
 
 // The workgroup numbers the positions with a target in order: each(position, has, number) for every position; returns how many there are.
 template <int THREADS, typename Each>
@@ -186,7 +186,11 @@ __device__ __forceinline__ Item logit_item(const Head &q, const bf16_t *op, int 
   return i;
 }
 
-// (max, sum of exponentials) of each row and group of vocabulary entries; the logit of the target from the tile that has it
+// (max, sum of exponentials) of each row and group of vocabulary entries; the product of the target from the tile that has it.  Maxima and the target's are
+// kept as the products they are, and only their differences are scaled: the largest entry's is exactly 0 at any temperature, its exponential 1, so that no
+// log-probability is above 0 and a certain token's is 0.  (A scaled maximum is rounded, by inv_t z 2^-24, and z inv_t - that is not 0.  An instruction a
+// logit more than the multiply-add takes; us, with that / so: 4096 positions of 152064 x 3584 2845 / 2853, of 32000 x 256 120.6 / 125.4, 61 of 151936 x 1536
+// 91.6 / 93.2.)
 // COLD: one tile of rows, so that W is read once.
 // DIRECT: few positions, which every workgroup numbers for itself and whose rows it takes as they lie, each lane from another: no launch ahead, and lanes
 // without a row load nothing.  us, with the gather / so: tiny shape 14.6 / 12.1, 1.5B 4 positions 89.9 / 79.7, 32 90.3 / 87.5, 48 90.7 / 95.7; 152064 x
@@ -269,20 +273,19 @@ __global__ __launch_bounds__(256) void loss_forward_kernel(Head q, Positions at,
           for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-              if (y - t.half * 4 == h * 32 + (i >> 2) * 8 + (i & 3) && r < count) zt[r] = z[h][i] * row.factor;
+              if (y - t.half * 4 == h * 32 + (i >> 2) * 8 + (i & 3) && r < count) zt[r] = z[h][i];
         }
         float m = z[0][0];
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
           for (int i = 0; i < 16; ++i) m = fmaxf(m, z[h][i]);
-        // (the rounding of m, which every difference shares, is in the sum too: m + log2 s is exact about it)
-        m = with_xor32(m, OpMax{}) * row.factor;
+        m = with_xor32(m, OpMax{});
         float s = 0.f;
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) s += __builtin_amdgcn_exp2f(fmaf(z[h][i], row.factor, -m));
+          for (int i = 0; i < 16; ++i) s += __builtin_amdgcn_exp2f((z[h][i] - m) * row.factor);
         s = with_xor32(s, OpSum{});
         if (t.half == 0 && r < count && v < q.vocab) parts[(int64_t)(v / GROUP) * n_pad + r] = make_float2(m, s);
 #ifdef __HIP_DEVICE_COMPILE__
@@ -296,17 +299,19 @@ __global__ __launch_bounds__(256) void loss_forward_kernel(Head q, Positions at,
 // The groups of JOIN_ROWS rows joined, by JOIN threads per row: each takes every JOINth group in order, then their results are joined, sixteen at a time and
 // the rest, in order.  (One number of threads for every call: a row's result is to be the same in all.)
 constexpr int JOIN_ROWS = 8, JOIN = 1024 / JOIN_ROWS;
-__global__ __launch_bounds__(1024) void loss_merge_kernel(const float2 *__restrict__ parts, const float *__restrict__ zt, const int32_t *__restrict__ rows,
-                                                          const Cut *__restrict__ cut, float *__restrict__ logprob, float *__restrict__ lse, int groups, int first,
-                                                          int n_pad) {
+__global__ __launch_bounds__(1024) void loss_merge_kernel(const float2 *__restrict__ parts, const float *__restrict__ zt, const float *__restrict__ inv_t,
+                                                          const int32_t *__restrict__ rows, const Cut *__restrict__ cut, float *__restrict__ logprob,
+                                                          float *__restrict__ lse, int groups, int first, int n_pad) {
   __shared__ float2 joined[JOIN][JOIN_ROWS];
   const int row = threadIdx.x % JOIN_ROWS, at = threadIdx.x / JOIN_ROWS, r = blockIdx.x * JOIN_ROWS + row, n = min(cut->count - first, n_pad);
   if ((int)blockIdx.x * JOIN_ROWS >= n) return;
+  const int t = r < n ? rows[first + r] : 0;
+  const float it = r < n && inv_t ? inv_t[t] : 1.f, factor = logit_factor(it);
   // (no entries: -inf, 0; NaN stays)
-  auto join = [](float &m, float &s, float2 p) {
+  auto join = [&](float &m, float &s, float2 p) {
     const float top = p.x > m || p.x != p.x ? p.x : m;
     if (top == -INFINITY) return;
-    s = s * __builtin_amdgcn_exp2f(m - top) + p.y * __builtin_amdgcn_exp2f(p.x - top);
+    s = s * __builtin_amdgcn_exp2f((m - top) * factor) + p.y * __builtin_amdgcn_exp2f((p.x - top) * factor);
     m = top;
   };
   const float2 none = make_float2(-INFINITY, 0.f);
@@ -330,10 +335,9 @@ __global__ __launch_bounds__(1024) void loss_merge_kernel(const float2 *__restri
     if (at < left) joined[at][row] = make_float2(m, s);
   }
   if (at || r >= n) return;
-  const float l = log2f(s);
-  const int t = rows[first + r];
-  lse[t] = (m + l) * LN2;
-  logprob[t] = ((zt[r] - m) - l) * LN2;   // (a certain token's logit is m, to the last bit)
+  const float l = log2f(s) * LN2;   // (s >= 1: the largest entry's own exponential)
+  lse[t] = fmaf(it, m, l);
+  logprob[t] = fmaf(it, zt[r] - m, -l);
 }
 
 // a 32 x 32 block of results (a lane: one column, rows (i / 4) * 8 + half * 4 + i % 4) as two fragments of eight consecutive rows: 16 f + 8 half on
@@ -713,7 +717,7 @@ int launch_token_logprob(const TokenLoss &p, float *logprob, float *lse, hipStre
   const Positions at{p.target, w.cut, w.rows, nullptr, logprob, lse, p.n, p.vocab, p.d, GRAD_MOST, p.ldw};
   const bool number = p.n <= NUMBER_MOST;
   auto merge = [&](int first) {
-    hipLaunchKernelGGL(loss_merge_kernel, dim3((std::min(p.n - first, w.n_pad) + JOIN_ROWS - 1) / JOIN_ROWS), dim3(1024), 0, s, w.parts, w.zt, w.rows, w.cut, logprob, lse,
+    hipLaunchKernelGGL(loss_merge_kernel, dim3((std::min(p.n - first, w.n_pad) + JOIN_ROWS - 1) / JOIN_ROWS), dim3(1024), 0, s, w.parts, w.zt, p.inv_t, w.rows, w.cut, logprob, lse,
                        w.groups, first, w.n_pad);
   };
   if (p.n <= DIRECT_MOST && (p.n * p.ldh + p.d) * 2 < 0x7fff0000) {   // (rows behind one 32-bit offset)
