@@ -281,11 +281,12 @@ __global__ __launch_bounds__(256) void loss_forward_kernel(Head q, Positions at,
 #pragma unroll
           for (int i = 0; i < 16; ++i) m = fmaxf(m, z[h][i]);
         m = with_xor32(m, OpMax{});
+        const float from = m == -INFINITY ? 0.f : m;   // (a group of -inf adds nothing: its exponentials are 0)
         float s = 0.f;
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) s += __builtin_amdgcn_exp2f((z[h][i] - m) * row.factor);
+          for (int i = 0; i < 16; ++i) s += __builtin_amdgcn_exp2f((z[h][i] - from) * row.factor);
         s = with_xor32(s, OpSum{});
         if (t.half == 0 && r < count && v < q.vocab) parts[(int64_t)(v / GROUP) * n_pad + r] = make_float2(m, s);
 #ifdef __HIP_DEVICE_COMPILE__
@@ -307,10 +308,13 @@ __global__ __launch_bounds__(1024) void loss_merge_kernel(const float2 *__restri
   if ((int)blockIdx.x * JOIN_ROWS >= n) return;
   const int t = r < n ? rows[first + r] : 0;
   const float it = r < n && inv_t ? inv_t[t] : 1.f, factor = logit_factor(it);
-  // (no entries: -inf, 0; NaN stays)
+  // (no entries, or none but -inf: -inf, 0; NaN stays, in the maximum or in the sum)
   auto join = [&](float &m, float &s, float2 p) {
     const float top = p.x > m || p.x != p.x ? p.x : m;
-    if (top == -INFINITY) return;
+    if (top == -INFINITY) {
+      s += p.y;
+      return;
+    }
     s = s * __builtin_amdgcn_exp2f((m - top) * factor) + p.y * __builtin_amdgcn_exp2f((p.x - top) * factor);
     m = top;
   };
