@@ -423,7 +423,8 @@ int pl_token_logprob(const void *h, int64_t ldh, const void *w, int64_t ldw, con
  * lse and the first six arguments are those of the forward call (lse device fp32 [n], g device fp32 [n]; neither is read where there is no
  * target).  The logits are computed again, piece by piece of the vocabulary; G is rounded to bf16 for the products (half a step, as the
  * operands are; calls of up to 128 positions keep a second bf16 term of it), sums are fp32, results are rounded once.  Results are the same bits
- * from call to call.  A NaN in g, lse or inv_temperature of a position with a target makes its row of dh NaN, and dw.
+ * from call to call.  A NaN in g, lse or inv_temperature of a position with a target, or an infinite lse, makes its row of dh NaN, and dw.  lse is a number
+ * of 32 bits: probabilities are off by half its last place (2^-24 |lse|, relative); where z[t, v] is that near to lse, the probability is taken for 1.
  * PL_E_INVAL as above, and for n * d * 2 bytes (n counted up to a multiple of 256) of 2 GiB or more, dh or dw not aligned to 16 bytes, neither asked for. */
 int64_t pl_token_logprob_grad_workspace_bytes(int32_t n, int32_t vocab, int32_t d);
 int pl_token_logprob_grad(const void *h, int64_t ldh, const void *w, int64_t ldw, const int32_t *target, const float *inv_temperature,

@@ -25,8 +25,10 @@ constexpr int PIECE = 8192;         // rows of a forward pass: 8 bytes per row a
 constexpr int UNITS = 256;          // workgroups of a kernel that walks tiles: one fills a compute unit
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
-// Exponentials are powers of two.  factor = inv_t log2(e), lse2 = lse log2(e), scale = g inv_t; padding: all 0, target -1
-struct Row { float factor, lse2, scale; int32_t target; };
+// What the tiles want of a row.  Forward: factor = inv_t log2(e), since exponentials are powers of two; gradient: factor = inv_t, lse, scale = g inv_t.
+// Padding: all 0, target -1.
+struct Row { float factor, lse, scale; int32_t target; };
+__device__ inline float finite_or_nan(float x) { return fabsf(x) < INFINITY ? x : NAN; }
 // (not negative: the largest product has the largest logit; of 0 the smallest normal number, whose logits are 0 beside any sum of exponentials: entries beyond
 // the vocabulary, -inf, stay that and do not become 0 * inf; finite, so that a difference of 0 stays one)
 __device__ inline float logit_factor(float inv_t) { return inv_t >= 0.f && inv_t < INFINITY ? fminf(fmaxf(inv_t * LOG2E, 0x1p-126f), 0x1.fffffep127f) : NAN; }
@@ -150,7 +152,11 @@ __global__ __launch_bounds__(256) void loss_gather_kernel(Head q, Positions at, 
     if (t >= 0) {
       const float inv_t = q.inv_t ? q.inv_t[t] : 1.f;
       i.factor = logit_factor(inv_t);
-      if (q.g) { i.lse2 = q.lse[t] * LOG2E; i.scale = q.g[t] * inv_t; }
+      if (q.g) {
+        i.factor = inv_t >= 0.f ? finite_or_nan(inv_t) : NAN;
+        i.lse = finite_or_nan(q.lse[t]);
+        i.scale = q.g[t] * inv_t;
+      }
       i.target = q.target[t];
     }
     info[r] = i;
@@ -399,12 +405,20 @@ __global__ __launch_bounds__(256) void loss_grad_logits_kernel(Head q, const bf1
     for (int b = 0; b < BT; ++b) {
       const int m32 = (c.row0 >> 5) + t.wn * BT + b;
       const Row row = info[m32 * 32 + t.lrow];
+      // lse is a rounded number: a logit within half its last place is lse, as far as that says, and the probability 1, so that a certain token has no
+      // gradient however large the logits are (otherwise 1.2e-6 of g at a logit of 20, but all of it and more from 1e7 on).  The multiple of inv_t is not
+      // rounded before lse is taken off.  us, by one multiply-add and an exponential / so: 4096 positions of 152064 x 3584 8618 / 8653, 777 of 151936 x 1536
+      // 668 / 677, 4096 of 32000 x 256 353 / 372.
+      const float near = fabsf(row.lse) * 0x1p-24f;
 #pragma unroll
       for (int a = 0; a < AT; ++a) {
         const int v = v0 + a * 32, v32 = (v - v_begin) >> 5, y = row.target - v;
         float G[16];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) G[i] = -row.scale * __builtin_amdgcn_exp2f(fmaf(t.result(a, b, i), row.factor, -row.lse2));
+        for (int i = 0; i < 16; ++i) {
+          const float x = fmaf(t.result(a, b, i), row.factor, -row.lse);
+          G[i] = -row.scale * __builtin_amdgcn_exp2f((fabsf(x) <= near ? 0.f : x) * LOG2E);
+        }
         if (__ballot(y >= 0 && y < 32)) {
 #pragma unroll
           for (int i = 0; i < 16; ++i)

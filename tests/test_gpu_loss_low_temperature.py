@@ -94,3 +94,65 @@ def test_the_largest_inverse_temperatures(n):
     lp, lse = c.results()
     assert (lp[target == top] == 0).all() and (lp[target != top] == -np.inf).all()
     assert (lse == np.inf).all()
+    c.backward(c.lse[:n].clone(), torch.ones(n, device="cuda"))
+    assert np.isnan(c.gradients()[0]).all()      # (an infinite lse says nothing of the probabilities)
+
+
+def gradients(h, w, target, it, g, lse):
+    """G, dh, dw in 64 bits; lse in 64 bits too."""
+    z = it[:, None].astype(np.float64) * (h.astype(np.float64) @ w.astype(np.float64).T)
+    G = -np.exp(z - lse[:, None])
+    G[np.arange(len(h)), target] += 1
+    G *= (g.astype(np.float64) * it)[:, None]
+    return G, G @ w.astype(np.float64), G.T @ h.astype(np.float64)
+
+
+@pytest.mark.parametrize("inv_t", [10.0, 1e3, 1e6, 1e9, 1e30])
+@pytest.mark.parametrize("n", ROWS)
+def test_gradients_where_one_token_is_certain(n, inv_t):
+    """A certain token's gradient vanishes, that of an impossible target is g inv_t (w[target] - w[certain]): whatever lse, a number of 32 bits, is off by."""
+    vocab, d = 700, 512
+    h, w, top, rng = exact_batch(n, vocab, d, n, 16)
+    target = np.where(rng.random(n) < 0.5, top, (top + 1 + rng.integers(0, vocab - 1, n)) % vocab)
+    it = np.full(n, inv_t, np.float32)
+    g = rng.normal(size=n).astype(np.float32)
+    c = Call(h, w, target, it)
+    c.forward()
+    c.backward(c.lse[:n].clone(), torch.from_numpy(g).cuda())
+    dh, dw = c.gradients()
+    _, true_lse, _, _ = reference(h, w, target, it)
+    G, ref_h, ref_w = gradients(h, w, target, it, g, true_lse)
+    # entries of G are g inv_t, minus it, or below 1e-40 of it; g inv_t is rounded (2^-24) and, to bf16, once more; sums and results as anywhere
+    G = np.where(np.abs(G) < 1e-30 * np.abs(g * it.astype(np.float64))[:, None], 0, G)
+    e_G = (2.0 ** -8 + 2.0 ** -23) * np.abs(G)
+    for got, ref, e in ((dh, G @ w, e_G @ np.abs(w) + (vocab + 64) * 2.0 ** -24 * (np.abs(G) @ np.abs(w))),
+                        (dw, G.T @ h, e_G.T @ np.abs(h) + (n + 64) * 2.0 ** -24 * (np.abs(G).T @ np.abs(h)))):
+        assert (np.abs(got - ref) <= e + 2.0 ** -8 * (np.abs(ref) + e) + 1e-38 * inv_t).all(), np.abs(got - ref).max() / inv_t
+    assert (np.abs(dh[target == top]) <= 1e-30 * inv_t).all()
+
+
+@pytest.mark.parametrize("n", [20, 100, 300])
+def test_gradients_of_far_logits(n):
+    """Logits of thousands at a temperature of one, and a row whose logits are all equal."""
+    vocab, d = 700, 512
+    h, w, top, rng = exact_batch(n, vocab, d, n, 16)
+    h *= 512
+    h[0] = 0
+    target = np.where(np.arange(n) % 2, top, (top + 7) % vocab)
+    it = np.ones(n, np.float32)
+    g = rng.normal(size=n).astype(np.float32)
+    c = Call(h, w, target, None)
+    c.forward()
+    lp, lse = c.results()
+    ref_lp, true_lse, e_lp, e_lse = reference(h, w, target, it)
+    assert (lp <= 0).all() and (np.abs(lp - ref_lp) <= e_lp).all() and (np.abs(lse - true_lse) <= e_lse).all()
+    c.backward(c.lse[:n].clone(), torch.from_numpy(g).cuda())
+    dh, dw = c.gradients()
+    G, ref_h, ref_w = gradients(h, w, target, it, g, true_lse)
+    # (of the row of equal logits: e^-lse is off by what lse, 6.6, is rounded by, and an exponential's 2^-20)
+    e_G = (2.0 ** -8 + 2.0 ** -19) * np.abs(G) + 2.0 ** -22 * np.abs(g)[:, None] * (np.abs(G) > 0)
+    for got, ref, e in ((dh, ref_h, e_G @ np.abs(w) + (vocab + 64) * 2.0 ** -24 * (np.abs(G) @ np.abs(w))),
+                        (dw, ref_w, e_G.T @ np.abs(h) + (n + 64) * 2.0 ** -24 * (np.abs(G).T @ np.abs(h)))):
+        assert (np.abs(got - ref) <= e + 2.0 ** -8 * (np.abs(ref) + e) + 1e-30).all(), np.abs(got - ref).max()
+    certain = (target == top) & (np.arange(n) > 0)
+    assert certain.any() and (np.abs(dh[certain]) <= 1e-30).all()
