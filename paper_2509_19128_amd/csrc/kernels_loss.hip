@@ -410,6 +410,7 @@ __global__ __launch_bounds__(256) void loss_grad_logits_kernel(Head q, const bf1
       // rounded before lse is taken off.  us, by one multiply-add and an exponential / so: 4096 positions of 152064 x 3584 8618 / 8653, 777 of 151936 x 1536
       // 668 / 677, 4096 of 32000 x 256 353 / 372.
       const float near = fabsf(row.lse) * 0x1p-24f;
+      const uint32_t keep = row.target < 0 ? 0u : ~0u;   // (padding is 0 whatever W holds: its logits are NaN where a weight is infinite)
 #pragma unroll
       for (int a = 0; a < AT; ++a) {
         const int v = v0 + a * 32, v32 = (v - v_begin) >> 5, y = row.target - v;
@@ -429,16 +430,18 @@ __global__ __launch_bounds__(256) void loss_grad_logits_kernel(Head q, const bf1
           for (int i = 0; i < 16; ++i)
             if ((i >> 2) * 8 + (i & 3) >= q.vocab - v - t.half * 4) G[i] = 0.f;
         }
-        uint4 f[2];
-        fragments(f, G);
+        auto write = [&](int block) {
+          uint4 f[2];
+          fragments(f, G);
 #pragma unroll
-        for (int k = 0; k < 2; ++k) *(uint4 *)((char *)G_out + fragment_place(m32, v32, n_rows, k, t.half, t.lrow)) = f[k];
+          for (int k = 0; k < 2; ++k)
+            *(uint4 *)((char *)G_out + fragment_place(block, v32, n_rows, k, t.half, t.lrow)) = make_uint4(f[k].x & keep, f[k].y & keep, f[k].z & keep, f[k].w & keep);
+        };
+        write(m32);
         if constexpr (SPLIT) {
 #pragma unroll
           for (int i = 0; i < 16; ++i) G[i] -= (float)(bf16_t)G[i];
-          fragments(f, G);
-#pragma unroll
-          for (int k = 0; k < 2; ++k) *(uint4 *)((char *)G_out + fragment_place(m32 + T::BN / 32, v32, n_rows, k, t.half, t.lrow)) = f[k];
+          write(m32 + T::BN / 32);
         }
 #ifdef __HIP_DEVICE_COMPILE__
         __builtin_amdgcn_sched_barrier(0);   // (one block's registers at a time)

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from test_gpu_loss import Call
-from test_gpu_loss_low_temperature import exact_batch, reference
+from test_gpu_loss_low_temperature import exact_batch, gradients, reference
 
 pytestmark = pytest.mark.gpu
 
@@ -69,3 +69,22 @@ def test_a_nan_beside_masked_entries_is_not_lost(n, entry):
     c.forward()
     lp, lse = c.results()
     assert np.isnan(lp).all() and np.isnan(lse).all()
+
+
+@pytest.mark.parametrize("mask", MASKS)
+@pytest.mark.parametrize("n", [1, 20, 60, 128, 200, 300])
+def test_masked_entries_have_no_gradient(n, mask):
+    """dw of masked entries is 0 and that of the others as without them, whatever rows the call is padded to.  (dh is G w: 0 times infinity.)"""
+    h, w, blocked, out, target, it, rng = masked_batch(n, MASKS[mask], 20 + n)
+    g = rng.normal(size=n).astype(np.float32)
+    c = Call(h, blocked, target, it)
+    c.forward()
+    c.backward(c.lse[:n].clone(), torch.from_numpy(g).cuda(), dh=False)
+    dw = c.gradients()[1]
+    _, ref_lse, _, _ = reference(h, w[~out], renumbered(out, target), it)
+    G, _, ref = gradients(h, w[~out], renumbered(out, target), it, g, ref_lse)
+    scale = np.abs(g * it)[:, None]
+    e_G = 2.0 ** -8 * np.abs(G) + 2.0 ** -18 * scale
+    e = e_G.T @ np.abs(h) + (n + 64) * 2.0 ** -24 * (np.abs(G).T @ np.abs(h))
+    assert (dw[out] == 0).all()
+    assert (np.abs(dw[~out] - ref) <= e + 2.0 ** -8 * (np.abs(ref) + e)).all()
