@@ -407,7 +407,8 @@ int pl_is_ess(const float *logp_pi, const float *logp_mu, const int64_t *seq_off
  *           0, and whatever its row of h holds (NaN included) reaches no other result.  Such positions cost nothing.
  *   inv_temperature  device fp32 [n], or NULL: 1.  0 makes all tokens equally likely; a negative one, an infinity or NaN gives its position NaN.
  *   logprob, lse     device fp32 [n] out
- *   workspace        device, at least pl_token_logprob_workspace_bytes(n, vocab, d) bytes, nothing of value in it afterwards
+ *   workspace        device, at least pl_token_logprob_workspace_bytes(n, vocab, d) bytes (which do for fewer positions too), nothing of value in it
+ *                    afterwards
  * bf16 products, fp32 sums.  A position's results do not depend on the other positions of the call, to the last bit.
  * PL_E_INVAL (nothing launched; the workspace size is then 0) for n or vocab below 1 or beyond 2^24, d not a multiple of 256 or beyond
  * 65536, a stride below d or not a multiple of 8 (ldw: beyond 2^20), h or w not aligned to 16 bytes.
@@ -445,8 +446,8 @@ int pl_quantize_int8(const void *w, int32_t dtype, int64_t ldw, void *w_q, float
  * w_q, w_scale from pl_quantize_int8.  With the codes xq, wq and the exact integer sum s = sum_k xq[m, k] wq[n, k]:
  *   y[m, n] = (float(s) * x_scale[m]) * w_scale[n], device [M, N] of y_dtype PL_F32 or PL_BF16 (rounded once more).
  * A row's results do not depend on the other rows of the call.  A row of x that holds an infinity or a NaN gives a row of NaN.
- * workspace: device, at least pl_gemm_int8_workspace_bytes(M, N, K) bytes, nothing of value in it afterwards; calls that overlap need
- * workspaces of their own.  PL_E_INVAL (nothing launched; the workspace size is then 0) for M < 1, N and K as above, M * K of 2 GiB or more,
+ * workspace: device, at least pl_gemm_int8_workspace_bytes(M, N, K) bytes (which do for fewer rows of the same N and K too), nothing of value
+ * in it afterwards; calls that overlap need workspaces of their own.  PL_E_INVAL (nothing launched; the workspace size is then 0) for M < 1, N and K as above, M * K of 2 GiB or more,
  * ldx below K or not a multiple of 8, x, w_q or y not aligned to 16 bytes.  Asynchronous on `stream` of the current device; may be
  * captured into a graph. */
 int64_t pl_gemm_int8_workspace_bytes(int32_t M, int32_t N, int32_t K);

@@ -489,6 +489,7 @@ constexpr ShapeTime SHAPES[] = {{32, 128, 5.29f, 0.275f, 0.137f, 0.128f, 0.217f,
                                 {128, 128, 7.75f, 0.359f, 0.289f, 0.278f, 0.313f, 2.88f, 0.386f, 0.098f}, {128, 256, 8.39f, 0.625f, 0.623f, 0.419f, 0.707f, 2.75f, 0.337f, 0.067f},
                                 {64, 64, 5.53f, 0.21f, 0.117f, 0.123f, 0.17f, 2.6f, 0.434f, 0.f},          {256, 256, 21.f, 0.98f, 0.393f, 0.407f, 1.258f, 0.f, 0.f, 0.377f}};
 struct Int8Plan { int shape, splits, slice; };
+constexpr int K_SLICES_MOST = 24, SLICED_TILES_MOST = 600;   // (the latter: tiles times slices)
 // gemm_int8_few_kernel, where a workgroup holds its rows in registers while it looks for their largest magnitudes: fixed (less 2 for the launches that the
 // caller's thread does not make), the quantisation, and a workgroup's part of W at what a unit gets, or all of W.  us, measured so / in two launches: 1 row 3584 x 3584 7.5 / 10.4, 37888 x 3584 22.9 / 28.8, 1536 x 8960
 // 12.3 / 11.1, 5120 x 27648 26.6 / 29.0; 4 rows 3584 x 3584 9.4 / 10.7, 37888 x 3584 23.5 / 29.0; 8 rows (a wavefront each) 16.2 / 11.2 and 29.1 / 30.4.
@@ -517,8 +518,8 @@ Int8Plan int8_plan(int M, int N, int K) {
     // tiles of mostly absent rows, and so many small ones that their W is read over and over, were not measured
     if ((f.rows > 64 && f.rows >= 4 * M) || (shape != I8_ROUNDS && (int64_t)f.rows * 24 < M)) continue;
     const int64_t tiles = (int64_t)((M + f.rows - 1) / f.rows) * ((N + f.cols - 1) / f.cols);
-    for (int sp : {1, 2, 3, 4, 5, 6, 8, 9, 12, 16, 24}) {
-      if (sp > groups || (sp > 1 && (shape == I8_ROUNDS || tiles * sp > 600))) break;
+    for (int sp : {1, 2, 3, 4, 5, 6, 8, 9, 12, 16, K_SLICES_MOST}) {
+      if (sp > groups || (sp > 1 && (shape == I8_ROUNDS || tiles * sp > SLICED_TILES_MOST))) break;
       const int per = (groups + sp - 1) / sp, splits = (groups + per - 1) / per;   // (no empty slice)
       const int64_t n = tiles * splits;
       const float r = n * (1.f / UNITS);
@@ -576,10 +577,18 @@ int launch_quantize_int8(const void *w, bool f32, int64_t ldw, int8_t *q, float 
   return done();
 }
 
+// Enough for every number of rows up to M: a program has one workspace for its largest batch, and fewer rows may take more slices.  With at most
+// SLICED_TILES_MOST tiles times slices, slices times rows of tiles are at most that over the tiles of a row.
 int64_t gemm_int8_workspace_bytes(int M, int N, int K) {
-  const Int8Plan p = int8_plan(M, N, K);
-  const int64_t codes = p.shape == I8_NARROW ? (int64_t)row_blocks(M) * 32 * K : (int64_t)M * ((K + K_UNIT - 1) / K_UNIT * K_UNIT);
-  return align256((int64_t)M * 4) + align256(codes) + (p.splits > 1 ? (int64_t)p.splits * M * N * 4 : 0);
+  const int groups = (K + K_UNIT - 1) / K_UNIT;
+  const int64_t ordered = N <= 16 * UNITS ? (int64_t)row_blocks(std::min(M, 64)) * 32 * K : 0;
+  int64_t sums = 0;
+#pragma unroll
+  for (int shape = 0; shape < I8_ROUNDS; ++shape) {
+    const int most = SLICED_TILES_MOST / ((N + SHAPES[shape].cols - 1) / SHAPES[shape].cols), slices = std::min({most, groups, K_SLICES_MOST});
+    if (slices > 1) sums = std::max(sums, std::min((int64_t)slices * M, (int64_t)most * SHAPES[shape].rows) * N);
+  }
+  return align256((int64_t)M * 4) + align256(std::max(ordered, (int64_t)M * groups * K_UNIT)) + sums * 4;
 }
 
 int launch_gemm_int8(const bf16_t *x, int64_t ldx, const int8_t *wq, const float *sw, void *y, bool f32, int M, int N, int K, void *ws, hipStream_t s) {
