@@ -453,6 +453,10 @@ int pl_quantize_int8(const void *w, int32_t dtype, int64_t ldw, void *w_q, float
 int64_t pl_gemm_int8_workspace_bytes(int32_t M, int32_t N, int32_t K);
 int pl_gemm_int8(const void *x, int64_t ldx, const void *w_q, const float *w_scale, void *y, int32_t y_dtype, int32_t M, int32_t N, int32_t K,
                  void *workspace, void *stream);
+/* How such a product is cut.  kernel: 0 to 4, a tile of rows x channels per workgroup (32 x 128, 64 x 128, 128 x 128, 128 x 256, 64 x 64); 5, tiles of
+ * 256 x 256 one after the other; 6, up to four rows in one launch; 7, up to 64 rows, 16 channels per workgroup.  splits: slices of K whose sums are added up
+ * by a launch of their own (1: none).  Either pointer may be NULL.  PL_E_INVAL for M, N and K that the product refuses. */
+int pl_debug_gemm_int8_plan(int32_t M, int32_t N, int32_t K, int32_t *kernel, int32_t *splits);
 
 #ifdef __cplusplus
 }

@@ -11,7 +11,7 @@ __all__ = [
     "PL_E_NOMEM", "PL_SWAP_ASYNC", "PL_SWAP_WAIT", "PL_SWAP_RECOMPUTE_KV", "PL_DEVICE_NONE", "PL_BF16", "PL_F32", "PL_GEMM_COLD", "PlError", "ModelCfg", "StepOut", "Stats",
     "lib", "library_path", "Engine", "operand_order", "pl_attention_decode", "pl_attention_workspace_bytes", "pl_kv_pack_host",
     "pl_gemm_bf16", "pl_debug_gemm_cfg", "pl_debug_gemm_plan", "pl_debug_gemm_planned", "pl_debug_gemm_folded", "pl_sample", "pl_sample_static", "pl_sample_workspace_bytes", "pl_debug_stream_read", "pl_is_ess",
-    "pl_token_logprob_workspace_bytes", "pl_token_logprob", "pl_token_logprob_grad_workspace_bytes", "pl_token_logprob_grad", "pl_quantize_int8", "pl_gemm_int8_workspace_bytes", "pl_gemm_int8", "EXPORTS",
+    "pl_token_logprob_workspace_bytes", "pl_token_logprob", "pl_token_logprob_grad_workspace_bytes", "pl_token_logprob_grad", "pl_quantize_int8", "pl_gemm_int8_workspace_bytes", "pl_gemm_int8", "pl_debug_gemm_int8_plan", "EXPORTS",
 ]
 
 PL_OK, PL_E_INVAL, PL_E_NOSLOT, PL_E_NOKV, PL_E_BUSY, PL_E_STATE, PL_E_CTX, PL_E_HIP, PL_E_NOMEM = 0, -1, -2, -3, -4, -5, -6, -7, -8
@@ -27,7 +27,7 @@ EXPORTS = [
     "pl_num_active", "pl_decode_step", "pl_get_stats", "pl_debug_get_logits", "pl_debug_read_kv",
     "pl_debug_write_kv", "pl_debug_add_sequence_at", "pl_debug_set_history", "pl_debug_set_poison", "pl_debug_set_graphs", "pl_debug_kv_pool", "pl_debug_set_profile", "pl_debug_gemm_cfg", "pl_debug_gemm_plan", "pl_debug_gemm_planned", "pl_debug_gemm_folded", "pl_debug_stream_read", "pl_attention_workspace_bytes",
     "pl_attention_decode", "pl_kv_pack_host", "pl_gemm_bf16", "pl_sample_workspace_bytes", "pl_sample", "pl_sample_static", "pl_is_ess",
-    "pl_token_logprob_workspace_bytes", "pl_token_logprob", "pl_token_logprob_grad_workspace_bytes", "pl_token_logprob_grad", "pl_quantize_int8", "pl_gemm_int8_workspace_bytes", "pl_gemm_int8",
+    "pl_token_logprob_workspace_bytes", "pl_token_logprob", "pl_token_logprob_grad_workspace_bytes", "pl_token_logprob_grad", "pl_quantize_int8", "pl_gemm_int8_workspace_bytes", "pl_gemm_int8", "pl_debug_gemm_int8_plan",
 ]
 
 
@@ -132,6 +132,7 @@ def lib():
         "pl_quantize_int8": (C.c_int, [vp, i32, i64, vp, vp, i32, i32, vp]),
         "pl_gemm_int8_workspace_bytes": (i64, [i32, i32, i32]),
         "pl_gemm_int8": (C.c_int, [vp, i64, vp, vp, vp, i32, i32, i32, i32, vp, vp]),
+        "pl_debug_gemm_int8_plan": (C.c_int, [i32, i32, i32, vp, vp]),
     }
     for name, (res, args) in sigs.items():
         fn = getattr(L, name)
@@ -472,3 +473,10 @@ def pl_gemm_int8_workspace_bytes(M, N, K):
 
 def pl_gemm_int8(x, ldx, w_q, w_scale, y, y_dtype, M, N, K, workspace, stream=0):
     _check(lib().pl_gemm_int8(x, ldx, w_q, w_scale, y, y_dtype, M, N, K, workspace, stream))
+
+
+def pl_debug_gemm_int8_plan(M, N, K):
+    """(kernel, splits) of such a product; see include/pl.h."""
+    kernel, splits = C.c_int32(), C.c_int32()
+    _check(lib().pl_debug_gemm_int8_plan(M, N, K, C.byref(kernel), C.byref(splits)))
+    return kernel.value, splits.value

@@ -591,6 +591,12 @@ int64_t gemm_int8_workspace_bytes(int M, int N, int K) {
   return align256((int64_t)M * 4) + align256(std::max(ordered, (int64_t)M * groups * K_UNIT)) + sums * 4;
 }
 
+void gemm_int8_plan(int M, int N, int K, int32_t *kernel, int32_t *splits) {
+  const Int8Plan p = int8_plan(M, N, K);
+  *kernel = p.shape;
+  *splits = p.splits;
+}
+
 int launch_gemm_int8(const bf16_t *x, int64_t ldx, const int8_t *wq, const float *sw, void *y, bool f32, int M, int N, int K, void *ws, hipStream_t s) {
   const Int8Plan plan = int8_plan(M, N, K);
   if (plan.shape == I8_FEW) {

@@ -290,6 +290,7 @@ int launch_token_logprob_grad(const TokenLoss &p, const float *lse, const float 
 // products in 8-bit integers (kernels_int8.hip)
 int launch_quantize_int8(const void *w, bool f32, int64_t ldw, int8_t *q, float *scale, int N, int K, hipStream_t s);
 int64_t gemm_int8_workspace_bytes(int M, int N, int K);
+void gemm_int8_plan(int M, int N, int K, int32_t *kernel, int32_t *splits);
 int launch_gemm_int8(const bf16_t *x, int64_t ldx, const int8_t *wq, const float *sw, void *y, bool f32, int M, int N, int K, void *ws, hipStream_t s);
 
 }  // namespace pl

@@ -1909,6 +1909,15 @@ int64_t pl_gemm_int8_workspace_bytes(int32_t M, int32_t N, int32_t K) {
   return pl::gemm_int8_workspace_bytes(M, N, K) + 256;
 }
 
+int pl_debug_gemm_int8_plan(int32_t M, int32_t N, int32_t K, int32_t *kernel, int32_t *splits) {
+  if (const char *why = int8_refusal(M, N, K)) return fail(PL_E_INVAL, "%s (M = %d, N = %d, K = %d)", why, M, N, K);
+  int32_t k, s;
+  pl::gemm_int8_plan(M, N, K, &k, &s);
+  if (kernel) *kernel = k;
+  if (splits) *splits = s;
+  return PL_OK;
+}
+
 int pl_gemm_int8(const void *x, int64_t ldx, const void *w_q, const float *w_scale, void *y, int32_t y_dtype, int32_t M, int32_t N, int32_t K,
                  void *workspace, void *stream) {
   if (!x || !w_q || !w_scale || !y || !workspace) return fail(PL_E_INVAL, "NULL argument");
