@@ -25,7 +25,8 @@ constexpr int PIECE = 8192;         // rows of a forward pass: 8 bytes per row a
 constexpr int UNITS = 256;          // workgroups of a kernel that walks tiles: one fills a compute unit
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
-// What the tiles want of a row.  Forward: factor = inv_t log2(e), since exponentials are powers of two; gradient: factor = inv_t, lse, scale = g inv_t.
+// What the tiles want of a row.  Forward: factor = inv_t log2(e), since exponentials are powers of two, scale = inv_t; gradient: factor = inv_t, lse,
+// scale = g inv_t.
 // Padding: all 0, target -1.
 struct Row { float factor, lse, scale; int32_t target; };
 __device__ inline float finite_or_nan(float x) { return fabsf(x) < INFINITY ? x : NAN; }
@@ -152,6 +153,7 @@ __global__ __launch_bounds__(256) void loss_gather_kernel(Head q, Positions at, 
     if (t >= 0) {
       const float inv_t = q.inv_t ? q.inv_t[t] : 1.f;
       i.factor = logit_factor(inv_t);
+      i.scale = inv_t;
       if (q.g) {
         i.factor = inv_t >= 0.f ? finite_or_nan(inv_t) : NAN;
         i.lse = finite_or_nan(q.lse[t]);
@@ -192,11 +194,11 @@ __device__ __forceinline__ Item logit_item(const Head &q, const bf16_t *op, int 
   return i;
 }
 
-// (max, sum of exponentials) of each row and group of vocabulary entries; the product of the target from the tile that has it.  Maxima and the target's are
+// (max, sum of exponentials) of each row and group of vocabulary entries; the product of the target (with inv_t) from the tile that has it.  Maxima and the target's are
 // kept as the products they are, and only their differences are scaled: the largest entry's is exactly 0 at any temperature, its exponential 1, so that no
 // log-probability is above 0 and a certain token's is 0.  (A scaled maximum is rounded, by inv_t z 2^-24, and z inv_t - that is not 0.  An instruction a
-// logit more than the multiply-add takes; us, with that / so: 4096 positions of 152064 x 3584 2845 / 2853, of 32000 x 256 120.6 / 125.4, 61 of 151936 x 1536
-// 91.6 / 93.2.)
+// logit more than the multiply-add takes; us, with that / so: 4096 positions of 152064 x 3584 2807 / 2806, of 32000 x 256 118.4 / 117.4, 61 of 151936 x 1536
+// 90.7 / 92.1.)
 // COLD: one tile of rows, so that W is read once.
 // DIRECT: few positions, which every workgroup numbers for itself and whose rows it takes as they lie, each lane from another: no launch ahead, and lanes
 // without a row load nothing.  us, with the gather / so: tiny shape 14.6 / 12.1, 1.5B 4 positions 89.9 / 79.7, 32 90.3 / 87.5, 48 90.7 / 95.7; 152064 x
@@ -204,13 +206,13 @@ __device__ __forceinline__ Item logit_item(const Head &q, const bf16_t *op, int 
 constexpr int DIRECT_MOST = 32;
 template <int WM, int WN, int AT, int BT, bool COLD, bool DIRECT>
 __global__ __launch_bounds__(256) void loss_forward_kernel(Head q, Positions at, const bf16_t *__restrict__ op, const Row *__restrict__ info, float2 *__restrict__ parts,
-                                                           float *__restrict__ zt, int first, int n_pad) {
+                                                           float2 *__restrict__ zt, int first, int n_pad) {
   typedef Tile<WM, WN, AT, BT, COLD, TILE_COLS, DIRECT> T;
   __shared__ __attribute__((aligned(1024))) bf16_t xs[T::LDS + (DIRECT ? 128 : 0)];
   int count;
   T t;
   t.init_at(xs);
-  float factor[BT];
+  float inv_ts[BT];
   int target[BT];
   if constexpr (DIRECT) {
     typedef __attribute__((address_space(3))) int32_t lds_int;
@@ -232,8 +234,7 @@ __global__ __launch_bounds__(256) void loss_forward_kernel(Head q, Positions at,
     for (int b = 0; b < BT; ++b) {
       const int r = (t.wn * BT + b) * 32 + t.lrow, row = r < count ? mine[r] : -1;
       t.row_w(b, row < 0 ? -1 : (int)(row * q.ldh));
-      const float inv_t = row >= 0 && q.inv_t ? q.inv_t[row] : 1.f;
-      factor[b] = logit_factor(inv_t);
+      inv_ts[b] = row >= 0 && q.inv_t ? q.inv_t[row] : 1.f;
       target[b] = row >= 0 ? q.target[row] : -1;
     }
   } else {
@@ -256,7 +257,7 @@ __global__ __launch_bounds__(256) void loss_forward_kernel(Head q, Positions at,
     for (int b = 0; b < BT; ++b) {
       const int r = c.row0 + (t.wn * BT + b) * 32 + t.lrow;
       Row row;
-      if constexpr (DIRECT) { row.factor = factor[b]; row.target = target[b]; }
+      if constexpr (DIRECT) { row.factor = logit_factor(inv_ts[b]); row.scale = inv_ts[b]; row.target = target[b]; }
       else row = info[r];
 #pragma unroll
       for (int a = 0; a < AT; a += 2) {
@@ -279,7 +280,7 @@ __global__ __launch_bounds__(256) void loss_forward_kernel(Head q, Positions at,
           for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-              if (y - t.half * 4 == h * 32 + (i >> 2) * 8 + (i & 3) && r < count) zt[r] = z[h][i];
+              if (y - t.half * 4 == h * 32 + (i >> 2) * 8 + (i & 3) && r < count) zt[r] = make_float2(z[h][i], row.scale);
         }
         float m = z[0][0];
 #pragma unroll
@@ -306,14 +307,14 @@ __global__ __launch_bounds__(256) void loss_forward_kernel(Head q, Positions at,
 // The groups of JOIN_ROWS rows joined, by JOIN threads per row: each takes every JOINth group in order, then their results are joined, sixteen at a time and
 // the rest, in order.  (One number of threads for every call: a row's result is to be the same in all.)
 constexpr int JOIN_ROWS = 8, JOIN = 1024 / JOIN_ROWS;
-__global__ __launch_bounds__(1024) void loss_merge_kernel(const float2 *__restrict__ parts, const float *__restrict__ zt, const float *__restrict__ inv_t,
-                                                          const int32_t *__restrict__ rows, const Cut *__restrict__ cut, float *__restrict__ logprob,
-                                                          float *__restrict__ lse, int groups, int first, int n_pad) {
+__global__ __launch_bounds__(1024) void loss_merge_kernel(const float2 *__restrict__ parts, const float2 *__restrict__ zt, const int32_t *__restrict__ rows,
+                                                          const Cut *__restrict__ cut, float *__restrict__ logprob, float *__restrict__ lse, int groups, int first,
+                                                          int n_pad) {
   __shared__ float2 joined[JOIN][JOIN_ROWS];
   const int row = threadIdx.x % JOIN_ROWS, at = threadIdx.x / JOIN_ROWS, r = blockIdx.x * JOIN_ROWS + row, n = min(cut->count - first, n_pad);
   if ((int)blockIdx.x * JOIN_ROWS >= n) return;
-  const int t = r < n ? rows[first + r] : 0;
-  const float it = r < n && inv_t ? inv_t[t] : 1.f, factor = logit_factor(it);
+  const float2 of_target = r < n ? zt[r] : make_float2(0.f, 0.f);   // its product, and inv_t
+  const float factor = logit_factor(of_target.y);
   // (no entries, or none but -inf: -inf, 0; NaN stays, in the maximum or in the sum)
   auto join = [&](float &m, float &s, float2 p) {
     const float top = p.x > m || p.x != p.x ? p.x : m;
@@ -346,8 +347,9 @@ __global__ __launch_bounds__(1024) void loss_merge_kernel(const float2 *__restri
   }
   if (at || r >= n) return;
   const float l = log2f(s) * LN2;   // (s >= 1: the largest entry's own exponential)
-  lse[t] = fmaf(it, m, l);
-  logprob[t] = fmaf(it, zt[r] - m, -l);
+  const int t = rows[first + r];
+  lse[t] = fmaf(of_target.y, m, l);
+  logprob[t] = fmaf(of_target.y, of_target.x - m, -l);
 }
 
 // a 32 x 32 block of results (a lane: one column, rows (i / 4) * 8 + half * 4 + i % 4) as two fragments of eight consecutive rows: 16 f + 8 half on
@@ -664,8 +666,7 @@ struct ForwardSpace {
   int32_t *rows;
   Row *info;
   bf16_t *op;
-  float *zt;
-  float2 *parts;
+  float2 *zt, *parts;
   int n_pad, groups;
   int64_t bytes;
   ForwardSpace(void *ws, int n, int vocab, int d) {
@@ -673,7 +674,7 @@ struct ForwardSpace {
     n_pad = padded(std::min(n, PIECE));
     groups = (vocab + GROUP - 1) / GROUP;
     cut = c.take<Cut>(1); rows = c.take<int32_t>(n); info = c.take<Row>(n_pad); op = c.take<bf16_t>((int64_t)n_pad * d);
-    zt = c.take<float>(n_pad); parts = c.take<float2>((int64_t)groups * n_pad);
+    zt = c.take<float2>(n_pad); parts = c.take<float2>((int64_t)groups * n_pad);
     bytes = c.at - (char *)ws;
   }
 };
@@ -738,7 +739,7 @@ int launch_token_logprob(const TokenLoss &p, float *logprob, float *lse, hipStre
   const Positions at{p.target, w.cut, w.rows, nullptr, logprob, lse, p.n, p.vocab, p.d, GRAD_MOST, p.ldw};
   const bool number = p.n <= NUMBER_MOST;
   auto merge = [&](int first) {
-    hipLaunchKernelGGL(loss_merge_kernel, dim3((std::min(p.n - first, w.n_pad) + JOIN_ROWS - 1) / JOIN_ROWS), dim3(1024), 0, s, w.parts, w.zt, p.inv_t, w.rows, w.cut, logprob, lse,
+    hipLaunchKernelGGL(loss_merge_kernel, dim3((std::min(p.n - first, w.n_pad) + JOIN_ROWS - 1) / JOIN_ROWS), dim3(1024), 0, s, w.parts, w.zt, w.rows, w.cut, logprob, lse,
                        w.groups, first, w.n_pad);
   };
   if (p.n <= DIRECT_MOST && (p.n * p.ldh + p.d) * 2 < 0x7fff0000) {   // (rows behind one 32-bit offset)
