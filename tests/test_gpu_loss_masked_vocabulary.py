@@ -88,3 +88,27 @@ def test_masked_entries_have_no_gradient(n, mask):
     e = e_G.T @ np.abs(h) + (n + 64) * 2.0 ** -24 * (np.abs(G).T @ np.abs(h))
     assert (dw[out] == 0).all()
     assert (np.abs(dw[~out] - ref) <= e + 2.0 ** -8 * (np.abs(ref) + e)).all()
+
+
+@pytest.mark.parametrize("mask", ["first group", "group 128", "last entries", "all but one", "every second"])
+@pytest.mark.parametrize("n", [1, 20, 60, 128, 300])
+def test_masks_of_the_lowest_number(n, mask):
+    """The lowest bf16 number as the weight: logits that an inverse temperature above 1 takes beyond fp32.  Here dh, with 0 times that number, is of the others."""
+    h, w, blocked, out, target, it, rng = masked_batch(n, MASKS[mask], 40 + n)
+    blocked[out, 5] = float(torch.finfo(torch.bfloat16).min)
+    g = rng.normal(size=n).astype(np.float32)
+    c = Call(h, blocked, target, it)
+    c.forward()
+    lp, lse = c.results()
+    left = renumbered(out, target)
+    ref_lp, ref_lse, e_lp, e_lse = reference(h, w[~out], left, it)
+    assert (np.abs(lp - ref_lp) <= e_lp).all() and (np.abs(lse - ref_lse) <= e_lse).all()
+    c.backward(c.lse[:n].clone(), torch.from_numpy(g).cuda())
+    dh, dw = c.gradients()
+    G, ref_h, ref_w = gradients(h, w[~out], left, it, g, ref_lse)
+    e_G = 2.0 ** -8 * np.abs(G) + 2.0 ** -18 * np.abs(g * it)[:, None]
+    e_h = e_G @ np.abs(w[~out]) + (VOCAB + 64) * 2.0 ** -24 * (np.abs(G) @ np.abs(w[~out]))
+    e_w = e_G.T @ np.abs(h) + (n + 64) * 2.0 ** -24 * (np.abs(G).T @ np.abs(h))
+    assert (dw[out] == 0).all()
+    assert (np.abs(dw[~out] - ref_w) <= e_w + 2.0 ** -8 * (np.abs(ref_w) + e_w)).all()
+    assert (np.abs(dh - ref_h) <= e_h + 2.0 ** -8 * (np.abs(ref_h) + e_h)).all()
