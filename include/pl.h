@@ -401,6 +401,8 @@ int pl_is_ess(const float *logp_pi, const float *logp_mu, const int64_t *seq_off
 /* Log-probabilities of given tokens under an LM head (the learner's log pi of recorded tokens, to set against the behaviour
  * log-prob in pl_is_ess), without logits in memory: with z[t, v] = inv_temperature[t] * sum_k h[t, k] w[v, k],
  *   lse[t] = log sum_v exp z[t, v],   logprob[t] = z[t, target[t]] - lse[t]    (the distribution that pl_sample records).
+ * Differences of logits are taken before inv_temperature multiplies them: no logprob is above 0, and a certain token's is 0, at any temperature (lse itself is
+ * infinite where inv_temperature[t] z passes the range of fp32).  An entry whose logits are -infinity is masked: its probability is 0.
  *   h       device bf16, n rows of d hidden states (behind the final norm), ldh elements apart
  *   w       device bf16, vocab rows of d weights, ldw elements apart: row-major, as a trainer (and a tied embedding table) has them
  *   target  device int32 [n].  A value outside [0, vocab) means a position without a target (prompts, padding): its logprob and lse are
@@ -422,10 +424,12 @@ int pl_token_logprob(const void *h, int64_t ldh, const void *w, int64_t ldw, con
  *   dh = G w   device bf16 [n, d], or NULL (not wanted); rows of positions without a target are 0
  *   dw = G^T h device bf16 [vocab, d], or NULL; every row is written
  * lse and the first six arguments are those of the forward call (lse device fp32 [n], g device fp32 [n]; neither is read where there is no
- * target).  The logits are computed again, piece by piece of the vocabulary; G is rounded to bf16 for the products (half a step, as the
- * operands are; calls of up to 128 positions keep a second bf16 term of it), sums are fp32, results are rounded once.  Results are the same bits
+ * target).  Workspace: pl_token_logprob_grad_workspace_bytes, otherwise as above.  The logits are computed again, piece by piece of the vocabulary;
+ * G is rounded to bf16 for the products (half a step, as the operands are: dh and dw are off by 2.4e-3 of their norm, where their own rounding makes 1.7e-3;
+ * calls of up to 128 positions keep a second bf16 term of it and only the latter), sums are fp32, results are rounded once.  Results are the same bits
  * from call to call.  A NaN in g, lse or inv_temperature of a position with a target, or an infinite lse, makes its row of dh NaN, and dw.  lse is a number
  * of 32 bits: probabilities are off by half its last place (2^-24 |lse|, relative); where z[t, v] is that near to lse, the probability is taken for 1.
+ * Entries that an infinite weight masks have rows of 0 in dw; dh, a product with that weight, is NaN (a mask of the lowest bf16 number leaves it right).
  * PL_E_INVAL as above, and for n * d * 2 bytes (n counted up to a multiple of 256) of 2 GiB or more, dh or dw not aligned to 16 bytes, neither asked for. */
 int64_t pl_token_logprob_grad_workspace_bytes(int32_t n, int32_t vocab, int32_t d);
 int pl_token_logprob_grad(const void *h, int64_t ldh, const void *w, int64_t ldw, const int32_t *target, const float *inv_temperature,

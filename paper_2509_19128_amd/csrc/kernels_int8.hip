@@ -491,7 +491,7 @@ constexpr ShapeTime SHAPES[] = {{32, 128, 5.29f, 0.275f, 0.137f, 0.128f, 0.217f,
 struct Int8Plan { int shape, splits, slice; };
 constexpr int K_SLICES_MOST = 24, SLICED_TILES_MOST = 600;   // (the latter: tiles times slices)
 // gemm_int8_few_kernel, where a workgroup holds its rows in registers while it looks for their largest magnitudes: fixed (less 2 for the launches that the
-// caller's thread does not make), the quantisation, and a workgroup's part of W at what a unit gets, or all of W.  us, measured so / in two launches: 1 row 3584 x 3584 7.5 / 10.4, 37888 x 3584 22.9 / 28.8, 1536 x 8960
+// caller's thread does not make), the quantisation, and a workgroup's part of W at what a unit gets, or all of W.  us, measured so / in two launches: 1 row 3584 x 3584 7.5 / 10.4, 37888 x 3584 22.9 / 28.8 (so, on other cards, 20.6 and 21.3), 1536 x 8960
 // 12.3 / 11.1, 5120 x 27648 26.6 / 29.0; 4 rows 3584 x 3584 9.4 / 10.7, 37888 x 3584 23.5 / 29.0; 8 rows (a wavefront each) 16.2 / 11.2 and 29.1 / 30.4.
 int few_rows(int M) { return M > 2 ? 4 : M; }
 bool few_fits(int M, int K) { return M <= 4 && few_rows(M) * K <= 512 * FEW_HELD * 8; }
