@@ -30,9 +30,11 @@ constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 // Padding: all 0, target -1.
 struct Row { float factor, lse, scale; int32_t target; };
 __device__ inline float finite_or_nan(float x) { return fabsf(x) < INFINITY ? x : NAN; }
-// (not negative: the largest product has the largest logit; of 0 the smallest normal number, whose logits are 0 beside any sum of exponentials: entries beyond
-// the vocabulary, -inf, stay that and do not become 0 * inf; finite, so that a difference of 0 stays one)
-__device__ inline float logit_factor(float inv_t) { return inv_t >= 0.f && inv_t < INFINITY ? fminf(fmaxf(inv_t * LOG2E, 0x1p-126f), 0x1.fffffep127f) : NAN; }
+// (not negative: the largest product has the largest logit; for 0 the smallest number, whose multiple of any product is below 5e-7, but of -inf, an entry that is masked
+// or beyond the vocabulary, -inf and not 0 * inf)
+__device__ inline float temperature(float inv_t) { return inv_t >= 0.f && inv_t < INFINITY ? fmaxf(inv_t, 0x1p-149f) : NAN; }
+// (finite, so that a difference of 0 stays one)
+__device__ inline float logit_factor(float it) { return it * LOG2E < INFINITY ? it * LOG2E : it == it ? 0x1.fffffep127f : NAN; }
 
 // The workgroup numbers the positions with a target in order: each(position, has, number) for every position; returns how many there are.
 template <int THREADS, typename Each>
@@ -151,11 +153,11 @@ __global__ __launch_bounds__(256) void loss_gather_kernel(Head q, Positions at, 
   if (blockIdx.y == 0 && threadIdx.x < 32) {
     Row i{0.f, 0.f, 0.f, -1};
     if (t >= 0) {
-      const float inv_t = q.inv_t ? q.inv_t[t] : 1.f;
-      i.factor = logit_factor(inv_t);
-      i.scale = inv_t;
+      const float inv_t = q.inv_t ? q.inv_t[t] : 1.f, it = temperature(inv_t);
+      i.factor = logit_factor(it);
+      i.scale = it;
       if (q.g) {
-        i.factor = inv_t >= 0.f ? finite_or_nan(inv_t) : NAN;
+        i.factor = it;
         i.lse = finite_or_nan(q.lse[t]);
         i.scale = q.g[t] * inv_t;
       }
@@ -234,7 +236,7 @@ __global__ __launch_bounds__(256) void loss_forward_kernel(Head q, Positions at,
     for (int b = 0; b < BT; ++b) {
       const int r = (t.wn * BT + b) * 32 + t.lrow, row = r < count ? mine[r] : -1;
       t.row_w(b, row < 0 ? -1 : (int)(row * q.ldh));
-      inv_ts[b] = row >= 0 && q.inv_t ? q.inv_t[row] : 1.f;
+      inv_ts[b] = temperature(row >= 0 && q.inv_t ? q.inv_t[row] : 1.f);
       target[b] = row >= 0 ? q.target[row] : -1;
     }
   } else {

@@ -112,3 +112,23 @@ def test_masks_of_the_lowest_number(n, mask):
     assert (dw[out] == 0).all()
     assert (np.abs(dw[~out] - ref_w) <= e_w + 2.0 ** -8 * (np.abs(ref_w) + e_w)).all()
     assert (np.abs(dh - ref_h) <= e_h + 2.0 ** -8 * (np.abs(ref_h) + e_h)).all()
+
+
+@pytest.mark.parametrize("n", [1, 20, 60, 128, 300])
+def test_masks_at_an_inverse_temperature_of_zero(n):
+    """All entries but those masked by an infinity are equally likely, those of the lowest number among them; nothing has a gradient."""
+    h, w, blocked, out, target, it, rng = masked_batch(n, slice(8192, 8400), 60 + n)
+    it[:] = 0.0
+    target[1::3] = 8200
+    for weight, left in ((-np.inf, VOCAB - 208), (float(torch.finfo(torch.bfloat16).min), VOCAB)):
+        blocked[out, 5] = weight
+        c = Call(h, blocked, target, it)
+        c.forward()
+        lp, lse = c.results()
+        of_masked = (target == 8200) & (weight == -np.inf)
+        # (a sum of ones, exact; a logarithm's 2^-22, and the lowest number's 5e-7)
+        assert (np.abs(lse - np.log(left)) <= 2.0 ** -22 * np.log(left) + 1e-6).all()
+        assert (np.abs(lp[~of_masked] + np.log(left)) <= 2.0 ** -22 * np.log(left) + 1e-6).all() and (lp[of_masked] == -np.inf).all()
+        c.backward(c.lse[:n].clone(), torch.ones(n, device="cuda"), dh=weight != -np.inf)
+        dh, dw = c.gradients()
+        assert (dw == 0).all() and (weight == -np.inf or (dh == 0).all())
