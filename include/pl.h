@@ -523,6 +523,7 @@ int pl_qk_norm_rope_grad(const void *qkv, int32_t dtype, int64_t ld, const void 
 /* pl_attention_decode through a window: row b sees positions j < ctx_len[b] with j < sinks or j >= ctx_len[b] - window.  Arguments as there, but: what hidden
  * positions hold (beyond ctx_len, or between the first ones and the window) plays no part, NaN included, and pages of which every position is hidden are not
  * read, nor is their entry of page_table used.  Contexts beyond max_ctx count as max_ctx; a row of none (ctx_len <= 0) is left as it was in out.
+ * Scores q . K are fp32: finite ones of any size have their softmax, one that overflows to +infinity gives its row NaN.
  * workspace: pl_attention_window_workspace_bytes bytes, nothing of value in it afterwards.  Up to two launches.
  * PL_E_INVAL (nothing launched; the workspace size is then 0) for n_seq outside [1, 1024], hd not 32, 64 or 128, more than 16 query heads per kv head or more than 1024 kv heads,
  * page_tokens not a positive multiple of 32, max_ctx < 1, beyond 2^30 or beyond pages_per_seq * page_tokens, window < 1, sinks < 0, q, kv_pages or out not aligned to 16 bytes. */

@@ -52,12 +52,16 @@ union Lds {               // (one object: with two, every read waits for the loa
 };
 typedef __attribute__((address_space(3))) void lds_void;
 
-// A maximum in powers of two, as the weights are taken relative to it: rounded, never part of a fused multiply-add, so that what is taken away from a score
-// and what a later maximum is compared with are one number.
-__device__ inline float in_powers(float m, float scale) {
-#pragma clang fp contract(off)
-  return m * scale;
+// Maxima are scores as the products leave them, and what is scaled is a difference of two of them, so that the largest weight is 1 whatever the scores are.  (Taken away from
+// a score's power of two, a maximum's, which is rounded to 32 bits, leaves half a step of it: more than 1 from 2^24 on, more than a weight can hold from 2^31 on.)
+// (m, l, o) <- (m, l, o) folded with a later part (mi, li, oi), the first part taken over as it is; a part without tokens has mi = -inf and changes nothing.
+__device__ inline void score_factors(float m, float mi, float scale, float &M, float &e0, float &e1) {
+  M = fmaxf(m, mi);
+  e0 = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - M) * scale);
+  e1 = mi == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mi - M) * scale);
 }
+template <int HD>
+__device__ inline float score_scale() { return 1.4426950408889634f / sqrtf((float)HD); }   // log2(e) / sqrt(hd)
 
 // Which positions of its context a row sees: those below `first` and those from `from` on.  Runs are counted without the hidden ones between.
 struct Sight {
@@ -82,7 +86,7 @@ template <int HD, int WAVES, typename F>
 __device__ __forceinline__ void attend_runs(const RangeAttn &p, Fold<HD, WAVES> &sm, int b, int g, const scalar_i32 *pages, const Sight &see, int v0, int v1, F put) {
   constexpr int NS = HD == 128 ? 2 : 4, NJ = HD / 32, NV = HD / 16;   // register stages of K and V; products of a tile of scores, of a run
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, head = l & 15, qg = l >> 4, G = p.Hq / p.Hkv;
-  const float scale = 1.4426950408889634f / sqrtf((float)HD);   // log2(e) / sqrt(hd)
+  const float scale = score_scale<HD>();
   const int64_t page_elems = (int64_t)2 * p.page_tokens * HD;
   const int n = v1 - v0, per_page = p.page_tokens >> 5;
   bf16x8 qf[NJ];
@@ -94,7 +98,7 @@ __device__ __forceinline__ void attend_runs(const RangeAttn &p, Fold<HD, WAVES> 
   f32x4 o[NV];
 #pragma unroll
   for (int i = 0; i < NV; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m = -INFINITY, m2 = -INFINITY, lsum = 0.f;   // the largest score, as it is and in powers of two
+  float m = -INFINITY, lsum = 0.f;   // the largest score
   bf16x8 kf[NS][2][NJ], vf[NS][NV];
   auto run_base = [&](int run, int page) { return p.kv + ((int64_t)page * p.Hkv + g) * page_elems + (int64_t)(run % per_page) * 32 * HD + l * 8; };
   auto load_k = [&](int st, const bf16_t *kb) {
@@ -154,18 +158,17 @@ __device__ __forceinline__ void attend_runs(const RangeAttn &p, Fold<HD, WAVES> 
 #pragma unroll
         for (int i = 0; i < NV; ++i) vf[st][i] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, vf[st][i]) & u32x4{keep[0], keep[1], keep[2], keep[3]});
       }
-      m = fmaxf(m, run_max(s));
-      const float ref = m == -INFINITY ? 0.f : in_powers(m, scale), alpha = __builtin_amdgcn_exp2f(m2 - ref);
+      const float top = fmaxf(m, run_max(s)), ref = top == -INFINITY ? 0.f : top, alpha = __builtin_amdgcn_exp2f((m - ref) * scale);
       float psum = 0.f;
       bf16x8 pf;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], scale, -ref));
+        const float w = __builtin_amdgcn_exp2f((s[e] - ref) * scale);
         psum += w;
         pf[e] = (__bf16)w;
       }
       lsum = __builtin_fmaf(lsum, alpha, psum);
-      m2 = m == -INFINITY ? m : ref;
+      m = top;
       if (__builtin_amdgcn_ballot_w64(!(alpha == 1.f))) {   // a maximum has moved (a factor of 1 changes nothing)
 #pragma unroll
         for (int i = 0; i < NV; ++i) o[i] *= alpha;
@@ -178,7 +181,7 @@ __device__ __forceinline__ void attend_runs(const RangeAttn &p, Fold<HD, WAVES> 
   lsum = column_sum(lsum);
 #pragma unroll
   for (int i = 0; i < NV; ++i) *(f32x4 *)&sm.o[wave][head][i * 16 + qg * 4] = o[i];
-  if (qg == 0) { sm.m[wave][head] = m2; sm.l[wave][head] = lsum; }
+  if (qg == 0) { sm.m[wave][head] = m; sm.l[wave][head] = lsum; }
   __syncthreads();
   for (int i = threadIdx.x; i < G * (HD / 4); i += WAVES * 64) {
     const int h = i / (HD / 4), d = i % (HD / 4) * 4;
@@ -190,7 +193,7 @@ __device__ __forceinline__ void attend_runs(const RangeAttn &p, Fold<HD, WAVES> 
     f32x4 O = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) {
-      const float f = __builtin_amdgcn_exp2f(sm.m[w][h] - ref);
+      const float f = __builtin_amdgcn_exp2f((sm.m[w][h] - ref) * scale);
       L = __builtin_fmaf(sm.l[w][h], f, L);
       O = fma4(*(const f32x4 *)&sm.o[w][h][d], f, O);
     }
@@ -237,7 +240,8 @@ struct Block {
   static constexpr int NJ = HD / 16, ND = HD / 32;
   bf16x8 qf[NJ];
   f32x16 o[ND];
-  float m2, lsum;   // what weights are relative to, in powers of two; the sum of the lane's weights
+  float m, off, lsum;   // the score that weights are relative to; its power of two, or 0 where scores have it taken away; the sum of the lane's weights
+  bool far;             // whether they have: a power of two of the wavefront's is 2^10 at least
 
   __device__ __forceinline__ void begin(const bf16_t *q, bool mine) {
 #pragma unroll
@@ -249,8 +253,9 @@ struct Block {
     for (int i = 0; i < ND; ++i)
 #pragma unroll
       for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
-    m2 = -INFINITY;
-    lsum = 0.f;
+    m = -INFINITY;
+    off = lsum = 0.f;
+    far = false;
   }
   // where a lane's fragments of a run are, behind its K and its V block's beginning
   __device__ static int in_k(int l) { return ((l & 16) / 16 * (HD / 8) + l / 32) * 128 + (l & 15) * 8; }   // + j * 256
@@ -266,31 +271,41 @@ struct Block {
   // What the weights of a run are relative to, and the factor of the sum so far.  The reference stays while no score is more than 2^8 above it (weights of up to 256 lose
   // nothing, in bf16 as in the sums): a maximum of 32 columns moves in nearly every run of a chunk, and the results' way through the vector unit is a
   // quarter of its time (64 rows of 5 heads over 16384 positions, 8 kv heads, this kernel alone: 44 -> 41 us).
-  __device__ __forceinline__ float2 peak(const f32x16 &s, float scale) {
+  // A weight is one fused operation and its power, relative to a power of two that was rounded by 2^-14 at most: next to nothing of a weight's own rounding.
+  // Larger ones would be rounded by more, in the end by more than a weight holds: there the maximum is taken away from the scores first.
+  __device__ __forceinline__ float peak(f32x16 &s, float scale) {
     float top = s[0];
 #pragma unroll
     for (int e = 1; e < 16; ++e) top = fmaxf(top, s[e]);
-    top = in_powers(with_xor32(top, OpMax{}), scale);
+    top = with_xor32(top, OpMax{});
     float alpha = 1.f;
-    const bool moves = top > m2 + 8.f;   // (the first run's: from -infinity)
+    const bool moves = top > m + 8.f / scale;   // (the first run's: from -infinity)
     if (__builtin_amdgcn_ballot_w64(moves)) {
-      const float ref = moves ? top : m2;
-      alpha = moves ? __builtin_amdgcn_exp2f(m2 - ref) : 1.f;
-      m2 = ref;
+      const float to = moves ? top : m;
+      alpha = moves ? __builtin_amdgcn_exp2f((m - to) * scale) : 1.f;
+      m = to;
+      off = m == -INFINITY ? 0.f : m * scale;
+      far = __builtin_amdgcn_ballot_w64(!(fabsf(off) < 1024.f));
+      if (far) off = 0.f;
 #pragma unroll
       for (int i = 0; i < ND; ++i) o[i] *= alpha;
     }
-    return make_float2(m2 == -INFINITY ? 0.f : m2, alpha);
+    if (far) {
+      const float from = m == -INFINITY ? 0.f : m;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] -= from;
+    }
+    return alpha;
   }
-  __device__ __forceinline__ void weigh(const f32x16 &s, float scale, float2 to, bf16x8 (&pf)[2]) {
+  __device__ __forceinline__ void weigh(const f32x16 &s, float scale, float alpha, bf16x8 (&pf)[2]) {
     float psum = 0.f;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {   // element e: token 16 (e / 4 % 2) + 8 (lane / 32) + 4 (e / 8) + e % 4 of the run
-      const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], scale, -to.x));
+      const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], scale, -off));
       psum += w;
       pf[e / 4 % 2][e / 8 * 4 + e % 4] = (__bf16)w;
     }
-    lsum = __builtin_fmaf(lsum, to.y, psum);
+    lsum = __builtin_fmaf(lsum, alpha, psum);
   }
   __device__ __forceinline__ void add(const bf16x8 (&vf)[ND][2], const bf16x8 (&pf)[2]) {
 #pragma unroll
@@ -313,7 +328,7 @@ __device__ __forceinline__ void attend_shared(const RangeAttn &p, Lds<HD> &lds, 
   const int col = wave % blocks * 32 + (l & 31), r = col / G, head = col % G;
   const bool mine = r < nrows;
   const int b = rows[mine ? r : 0];
-  const float scale = 1.4426950408889634f / sqrtf((float)HD);
+  const float scale = score_scale<HD>();
   const int64_t page_elems = (int64_t)2 * p.page_tokens * HD;
   const int per_page = p.page_tokens >> 5;
   Block<HD> x;
@@ -359,7 +374,7 @@ __device__ __forceinline__ void attend_shared(const RangeAttn &p, Lds<HD> &lds, 
       for (int j = 0; j < NJ; ++j) kf[j] = *(const bf16x8 *)(kb + j * 256);
     };
     // one run; the next one's scores are under way on the matrix cores while this one's are weighed
-    auto step = [&](int i, const f32x16 &s, f32x16 &s_next) {
+    auto step = [&](int i, f32x16 &s, f32x16 &s_next) {
       // run i + 1 has arrived, and every wavefront is done with run i - 1
       asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"i"(LOADS) : "memory");
       __builtin_amdgcn_s_barrier();
@@ -373,10 +388,10 @@ __device__ __forceinline__ void attend_shared(const RangeAttn &p, Lds<HD> &lds, 
       for (int k = 0; k < ND; ++k)
 #pragma unroll
         for (int q = 0; q < 2; ++q) vf[k][q] = *(const bf16x8 *)(vb + k * 1024 + q * 256);
-      const float2 to = x.peak(s, scale);
+      const float alpha = x.peak(s, scale);
       __builtin_amdgcn_s_setprio(1);   // before the other workgroup's reads and barriers (64 rows of 5 heads, 131072 shared positions, 8 kv heads, the call 234 -> 221 us)
       s_next = x.scores(kf);
-      x.weigh(s, scale, to, pf);
+      x.weigh(s, scale, alpha, pf);
       x.add(vf, pf);
       // weights between the products: a wavefront issues in order
 #pragma unroll
@@ -431,7 +446,7 @@ __device__ __forceinline__ void attend_shared(const RangeAttn &p, Lds<HD> &lds, 
     }
     int page = first + turns < r1 ? pages[(first + turns) / per_page] : 0;
     for (int run = first; run < r1; run += turns) {
-      const f32x16 s = x.scores(kf);
+      f32x16 s = x.scores(kf);
       const int nxt = run + turns;
       const bf16_t *nb = nullptr;
       if (nxt < r1) {
@@ -440,7 +455,8 @@ __device__ __forceinline__ void attend_shared(const RangeAttn &p, Lds<HD> &lds, 
         page = nxt + turns < r1 ? pages[(nxt + turns) / per_page] : 0;
       }
       bf16x8 pf[2];
-      x.weigh(s, scale, x.peak(s, scale), pf);
+      const float alpha = x.peak(s, scale);
+      x.weigh(s, scale, alpha, pf);
       x.add(vf, pf);
       if (nb) load_v(nb);
     }
@@ -456,15 +472,15 @@ __device__ __forceinline__ void attend_shared(const RangeAttn &p, Lds<HD> &lds, 
       for (int i = 0; i < ND; ++i)
 #pragma unroll
         for (int e = 0; e < 16; e += 4) *(f32x4 *)&so[at][cc][i * 32 + e * 2 + half * 4] = x.four(i, e);
-      if (half == 0) { sml[at][cc][0] = x.m2; sml[at][cc][1] = x.lsum; }
+      if (half == 0) { sml[at][cc][0] = x.m; sml[at][cc][1] = x.lsum; }
     }
     __syncthreads();
     if (turn < left / 2) {
       const int from = wave & 1;
       float M, e0, e1;
-      fold_factors(x.m2, sml[from][cc][0], M, e0, e1);
+      score_factors(x.m, sml[from][cc][0], scale, M, e0, e1);
       x.lsum = fold_value(x.lsum, e0, sml[from][cc][1], e1);
-      x.m2 = M;
+      x.m = M;
 #pragma unroll
       for (int i = 0; i < ND; ++i)
 #pragma unroll
@@ -483,7 +499,7 @@ __device__ __forceinline__ void attend_shared(const RangeAttn &p, Lds<HD> &lds, 
   for (int i = 0; i < ND; ++i)
 #pragma unroll
     for (int e = 0; e < 16; e += 4) *(f32x4 *)(to + i * 32 + e * 2 + half * 4) = x.four(i, e);
-  if (half == 0) *(float2 *)(parts.ml + part * ATTN_ML + head * 2) = make_float2(x.m2, x.lsum);
+  if (half == 0) *(float2 *)(parts.ml + part * ATTN_ML + head * 2) = make_float2(x.m, x.lsum);
 }
 
 // A workgroup an item, and more where there are more than 4096 (workgroups without one cost nothing: 512 to 100000 the same time; 512 that draw items from a counter
@@ -613,6 +629,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(RangeAttn p, MergeRows q
   const int ctx = min(p.ctx_len[b], p.max_ctx);
   if (ctx <= 0) return;
   const int64_t row = (int64_t)b * p.Hkv + g;
+  const float scale = score_scale<HD>();
   int n1 = 0, n2;
   auto put = [&](int i, float L, f32x4 O) { *(bf16x4 *)(p.out + ((int64_t)b * p.Hq + g * G) * HD + i * 4) = finish(O, L); };
   auto load = [&](const Parts &from, int c, int i, float2 &ml, f32x4 &o) {
@@ -636,11 +653,18 @@ __global__ __launch_bounds__(256) void attn_join_kernel(RangeAttn p, MergeRows q
   for (int i = threadIdx.x; i < G * (HD / 4); i += 256) {
     float M = -INFINITY, L = 0.f;
     f32x4 O = {0.f, 0.f, 0.f, 0.f};
+    auto fold = [&](float2 ml, f32x4 o) {
+      float top, e0, e1;
+      score_factors(M, ml.x, scale, top, e0, e1);
+      O = fold_value(O, e0, o, e1);
+      L = fold_value(L, e0, ml.y, e1);
+      M = top;
+    };
     int c0 = 0;
     if (early && i == (int)threadIdx.x) {
 #pragma unroll
       for (int u = 0; u < 8; ++u)
-        if (u < n1) fold_part(M, L, O, ml[u].x, ml[u].y, o[u]);
+        if (u < n1) fold(ml[u], o[u]);
       c0 = min(n1, 8);
     }
     for (; c0 < n1 + n2; c0 += 8) {
@@ -651,7 +675,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(RangeAttn p, MergeRows q
       }
 #pragma unroll
       for (int u = 0; u < 8; ++u)
-        if (c0 + u < n1 + n2) fold_part(M, L, O, ml[u].x, ml[u].y, o[u]);
+        if (c0 + u < n1 + n2) fold(ml[u], o[u]);
     }
     put(i, L, O);
   }
