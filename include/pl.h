@@ -524,7 +524,8 @@ int pl_qk_norm_rope_grad(const void *qkv, int32_t dtype, int64_t ld, const void 
  * positions hold (beyond ctx_len, or between the first ones and the window) plays no part, NaN included, and pages of which every position is hidden are not
  * read, nor is their entry of page_table used.  Contexts beyond max_ctx count as max_ctx; a row of none (ctx_len <= 0) is left as it was in out.
  * Scores q . K are fp32: finite ones of any size have their softmax, one that overflows to +infinity gives its row NaN.
- * workspace: pl_attention_window_workspace_bytes bytes, nothing of value in it afterwards.  Up to two launches.
+ * workspace: pl_attention_window_workspace_bytes bytes (which do for fewer rows, shorter contexts and windows and fewer first positions too), nothing of value in it
+ * afterwards.  Up to two launches.
  * PL_E_INVAL (nothing launched; the workspace size is then 0) for n_seq outside [1, 1024], hd not 32, 64 or 128, more than 16 query heads per kv head or more than 1024 kv heads,
  * page_tokens not a positive multiple of 32, max_ctx < 1, beyond 2^30 or beyond pages_per_seq * page_tokens, window < 1, sinks < 0, q, kv_pages or out not aligned to 16 bytes. */
 int64_t pl_attention_window_workspace_bytes(int32_t n_seq, int32_t n_q_heads, int32_t n_kv_heads, int32_t hd, int32_t max_ctx, int32_t window, int32_t sinks);
@@ -542,7 +543,8 @@ int pl_attention_window(const void *q, const void *kv_pages, const int32_t *page
  *                  context is shorter than those runs attends by itself.
  * Offsets that do not ascend or leave [0, n_seq] make no groups.  The result is the softmax over the whole context, as if nothing were shared; a row's bits depend
  * on n_seq, n_groups, max_ctx, max_shared, its group's shared_len, how many rows share it and its place among them, not on what the other rows hold.
- * workspace: pl_attention_shared_workspace_bytes bytes, nothing of value in it afterwards.  Up to three launches.  PL_E_INVAL (nothing launched; the workspace
+ * workspace: pl_attention_shared_workspace_bytes bytes (which do for fewer rows and groups, a smaller max_ctx and a smaller max_shared too), nothing of value in it
+ * afterwards.  Up to three launches.  PL_E_INVAL (nothing launched; the workspace
  * size is then 0) as above, for n_groups outside [1, n_seq], max_shared outside [0, max_ctx], and more than 2^30 work items. */
 int64_t pl_attention_shared_workspace_bytes(int32_t n_seq, int32_t n_groups, int32_t n_q_heads, int32_t n_kv_heads, int32_t hd, int32_t max_ctx, int32_t max_shared);
 int pl_attention_shared(const void *q, const void *kv_pages, const int32_t *page_table, const int32_t *ctx_len, const int32_t *group_offsets,

@@ -728,6 +728,14 @@ Split window_split(int n_seq, int Hkv, int hd, int max_ctx, int window, int sink
   return s;
 }
 
+// Most parts of any windowed call of as many pairs and runs or fewer, so that a workspace does for those too: fewer rows are cut into more chunks.  Chunks squared stay
+// below twice the runs; a call of up to 256 pairs (a whole window: 1024) has as many parts at most, one of up to 352 pairs four a pair.
+int64_t most_window_parts(int64_t pairs, int64_t runs) {
+  int64_t chunks = 1;
+  while (chunks < 1024 && (chunks + 1) * (chunks + 1) <= 2 * runs) ++chunks;
+  return std::max(chunks > 1 ? std::min<int64_t>(1024, pairs * chunks) : 0, pairs > 256 && runs >= 48 ? 4 * std::min<int64_t>(pairs, 352) : 0);
+}
+
 // How a call with shared prompts is cut: by its shape alone, so that a row's result does not depend on what the other rows hold.  A row's own part
 // goes in chunks of up to 64 runs (16 prompts of 2048 with 16 rollouts each, 7B shape: chunks of 16, 32, 64 and 128 runs 165, 158, 155 and 155 us) and
 // at least 16 (32 rows of 4 prompts of 1000 and 300 on average, 7B shape: by 4, 8 and 16 runs 23.1, 21.6 and 20.8).  Shared runs are cut
@@ -755,6 +763,21 @@ SharedSplit shared_split(int n_seq, int n_groups, int Hq, int Hkv, int hd, int m
   return s;
 }
 
+// The largest number of parts and items of any call of as many rows, groups and positions or fewer.  Own parts: chunks of less than 64 runs are taken where those of twice
+// the length would be less than 2048.  Shared parts: chunks squared stay below twice the runs, and they are 512 / units at most, or 1; units are a kv head's groups at least, and its tiles.
+struct SharedMost { int64_t own_parts, shared_parts, cap; };
+SharedMost most_shared(int n_seq, int n_groups, int Hq, int Hkv, int max_ctx, int max_shared) {
+  const int64_t pairs = (int64_t)n_seq * Hkv, tile_rows = 128 / (Hq / Hkv), runs = std::max(1, max_shared / 32);
+  int64_t chunks = 1;
+  while (chunks < 512 && (chunks + 1) * (chunks + 1) <= 2 * runs) ++chunks;
+  SharedMost m;
+  m.own_parts = std::max(pairs * up(max_ctx, 64 * 32), std::min<int64_t>(4096, pairs * up(max_ctx, 16 * 32)));
+  m.shared_parts = std::min(pairs * chunks, std::max(pairs, 512 * tile_rows));
+  const int64_t tiles = n_groups + n_seq / tile_rows;
+  m.cap = std::min(tiles * chunks, std::max<int64_t>(tiles, 1024 / Hkv)) + up(m.own_parts, Hkv);
+  return m;
+}
+
 int64_t part_floats(int G, int hd) { return (int64_t)G * hd + ATTN_ML; }
 Parts take_parts(float *&at, const Split &s, int G, int hd) {
   Parts r{at, at + s.parts * G * hd, s.chunks};
@@ -769,7 +792,7 @@ bool shared_fits(int n_seq, int n_groups, int Hq, int Hkv, int hd, int max_ctx, 
 }
 
 int64_t window_workspace_bytes(int n_seq, int Hq, int Hkv, int hd, int max_ctx, int window, int sinks) {
-  return window_split(n_seq, Hkv, hd, max_ctx, window, sinks).parts * part_floats(Hq / Hkv, hd) * 4;
+  return most_window_parts((int64_t)n_seq * Hkv, window_runs(max_ctx, window, sinks)) * part_floats(Hq / Hkv, hd) * 4;
 }
 
 int launch_attention_window(const RangeAttn &p, int window, int sinks, void *workspace, hipStream_t s) {
@@ -801,9 +824,10 @@ static bool shared_alone(int n_seq, int n_groups, int Hkv, int hd, int max_ctx, 
 }
 
 int64_t shared_workspace_bytes(int n_seq, int n_groups, int Hq, int Hkv, int hd, int max_ctx, int max_shared) {
-  if (shared_alone(n_seq, n_groups, Hkv, hd, max_ctx, max_shared)) return window_workspace_bytes(n_seq, Hq, Hkv, hd, max_ctx, max_ctx, 0);
-  const SharedSplit sp = shared_split(n_seq, n_groups, Hq, Hkv, hd, max_ctx, max_shared);
-  return (shared_ints(n_seq, sp.cap) + (sp.own.parts + sp.shared.parts) * part_floats(Hq / Hkv, hd)) * 4;
+  const int64_t alone = window_workspace_bytes(n_seq, Hq, Hkv, hd, max_ctx, max_ctx, 0);
+  if (shared_alone(n_seq, 1, Hkv, hd, max_ctx, max_shared)) return alone;   // (as are all smaller calls)
+  const SharedMost m = most_shared(n_seq, n_groups, Hq, Hkv, max_ctx, max_shared);
+  return std::max(alone, (shared_ints(n_seq, m.cap) + (m.own_parts + m.shared_parts) * part_floats(Hq / Hkv, hd)) * 4);
 }
 
 int launch_attention_shared(const RangeAttn &p, const SharedPrompts &q, void *workspace, hipStream_t s) {
