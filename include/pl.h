@@ -329,7 +329,7 @@ int64_t pl_debug_stream_read(const void *device_ptr, int64_t nbytes, int32_t non
  *              ((r * (hd / 16) + d / 16) * 4 + u / 8) * 128 + (d % 16) * 8 + u % 8.
  *   page_table device int32 [n_seq, pages_per_seq]; ctx_len device int32 [n_seq] (0 = skip row)
  *   out        device bf16 [n_seq, n_q_heads, hd]
- *   workspace  device, at least pl_attention_workspace_bytes(...) bytes
+ *   workspace  device, at least pl_attention_workspace_bytes(...) bytes (which do for fewer rows and a smaller max_ctx too)
  * max_ctx bounds ctx_len (sizes the launch).  Positions at or beyond ctx_len inside the last page
  * must hold finite values.  Up to three launches on `stream` (work list from ctx_len and page_table, the
  * attention proper, and, when max_ctx allows sequences of several chunks, their merge); the caller owns every buffer, the

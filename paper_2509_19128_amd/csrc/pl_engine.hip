@@ -1660,8 +1660,10 @@ static bool attention_direct(int32_t n_seq, int32_t n_kv_heads, int64_t max_chun
 
 int64_t pl_attention_workspace_bytes(int32_t n_seq, int32_t n_q_heads, int32_t n_kv_heads, int32_t hd, int32_t max_ctx) {
   if (n_seq < 1 || n_q_heads < 1 || n_kv_heads < 1 || hd < 1 || max_ctx < 1) return 0;
-  const int chunk = pl::attention_chunk_tokens(n_seq, n_kv_heads, max_ctx);
-  const int64_t max_chunks = (max_ctx + chunk - 1) / chunk, np = (int64_t)n_seq * max_chunks;
+  // the parts of any call with as many rows and positions or fewer: whole chunks, or shorter ones (of 128 tokens at least), which are taken where those of twice the
+  // length would be less than 2048 over all kv heads
+  const auto parts = [&](int64_t chunk) { return n_seq * ((max_ctx + chunk - 1) / chunk); };
+  const int64_t np = std::max(parts(pl::attention_chunk_tokens(1024, 1 << 20, max_ctx)), std::min<int64_t>(4096 / n_kv_heads, parts(128)));
   return np * n_q_heads * hd * 4 + np * n_kv_heads * pl::ATTN_ML * 4 + (pl::attention_worklist_ints(np) + (int64_t)n_seq * n_kv_heads) * 4 + 128;
 }
 

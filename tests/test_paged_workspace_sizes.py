@@ -17,6 +17,15 @@ def _growing(sizes):
 
 
 @pytest.mark.parametrize("Hq,Hkv,hd", HEADS)
+def test_decode(Hq, Hkv, hd):
+    size = pl.pl_attention_workspace_bytes
+    for n in (1, 3, 15, 16, 17, 31, 32, 89, 256, 1024):
+        _growing(size(n, Hq, Hkv, hd, c) for c in LENGTHS)
+    for most in LENGTHS:
+        _growing(size(n, Hq, Hkv, hd, most) for n in ROWS)
+
+
+@pytest.mark.parametrize("Hq,Hkv,hd", HEADS)
 def test_window(Hq, Hkv, hd):
     size = pl.pl_attention_window_workspace_bytes
     for n in (1, 3, 16, 31, 32, 65, 70, 89, 256, 300, 1024):
