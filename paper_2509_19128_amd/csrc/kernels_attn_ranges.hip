@@ -16,7 +16,7 @@ namespace {
 typedef __attribute__((address_space(4))) int32_t scalar_i32;   // read by scalar loads
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
-constexpr int ITEM_INTS = 8;   // of a work item's record: {kind, row or first of the rows, chunk, context or shared runs, first run or rows, row whose pages are read}
+constexpr int ITEM_INTS = 8;   // of a work item's record: {kind, row or first of the rows, chunk, context or shared runs, first run or rows, row whose pages are read, shared runs of a chunk}
                                // (with the ids of its first pages the list takes 1.7 us longer, and the items' first loads hide all of it: calls 2 us longer)
 constexpr int HEAD_INTS = 64;
 constexpr int64_t MOST_ITEMS = 1 << 30;   // a workgroup's next item stays below 2^31
@@ -26,11 +26,36 @@ struct Parts {
   float *o, *ml;           // of row b, kv head g, chunk c: element ((b Hkv + g) max_chunks + c) of [G, HD] and of [ATTN_ML]
   int32_t max_chunks;
 };
+// How a group's shared runs are cut, by their number: into as many chunks as make 256 workgroups, 384 from from[0] runs on, 512 from from[1] on, but into fewer, of about own_runs, where
+// rows' own parts keep the chip busy meanwhile.  Quotients by a reciprocal are put right, and no more than a step off: they are 512 at most.  (One workgroup does this while its
+// first loads are under way; by four divisions it takes 0.8 us longer.)
+struct SharedCut {
+  Divisor by[3];
+  int32_t from[2], own_runs;
+  __device__ static int up4(int a) { return (a + 3) & ~3; }
+  __device__ int chunk(int runs, int &chunks) const {
+    // (the three read ahead of the choice: a choice between their places would be read behind it)
+    const uint32_t m0 = __builtin_amdgcn_readfirstlane(by[0].m), m1 = __builtin_amdgcn_readfirstlane(by[1].m), m2 = __builtin_amdgcn_readfirstlane(by[2].m);
+    const uint32_t s0 = __builtin_amdgcn_readfirstlane(by[0].shift), s1 = __builtin_amdgcn_readfirstlane(by[1].shift), s2 = __builtin_amdgcn_readfirstlane(by[2].shift);
+    Divisor d;
+    d.m = runs >= from[1] ? m2 : runs >= from[0] ? m1 : m0;
+    d.shift = runs >= from[1] ? s2 : runs >= from[0] ? s1 : s0;
+    const int even = d.of(runs - 1);   // (runs of an even cut, and one more)
+    int c = max(up4(even + 1), up4((int)(__builtin_amdgcn_sqrtf(0.5f * (float)runs) + 0.99f)));   // (squared half of the runs at least, as for windows; 8 rollouts of one prompt of 16384, 7B shape, 33 -> 30 us)
+    c = min(max(c, max(8, own_runs)), up4(runs));
+    chunks = (int)((float)runs * __builtin_amdgcn_rcpf((float)c));
+    chunks += chunks * (int64_t)c < runs ? 1 : (chunks - 1) * (int64_t)c >= runs ? -1 : 0;
+    const int same = up4((int)((float)runs * __builtin_amdgcn_rcpf((float)chunks)) + 1);   // chunks of one length
+    return same < c && (int64_t)same * chunks >= runs ? same : c;
+  }
+};
 struct SharedWork {
   int32_t *head;                   // the number of items; behind it
-  int32_t *items, *rows, *start;   // records; rows that share, group by group; first run of a row's own part
+  int32_t *items, *rows;           // records; rows that share, group by group
+  int2 *start;                     // of every row: first run of its own part, shared parts before it
   Parts own, shared;
-  int32_t own_runs, shared_runs;   // of a chunk
+  int32_t own_runs;                // of a chunk
+  SharedCut cut;
   int32_t tile_rows, cap;
 };
 
@@ -515,13 +540,13 @@ __global__ __launch_bounds__(256, 2) void attn_shared_kernel(RangeAttn p, Shared
     if (item != (int)blockIdx.x) __syncthreads();   // LDS is free
     const int g = item % p.Hkv;
     const scalar_i32 *rec = (const scalar_i32 *)(w.items + (int64_t)(item / p.Hkv) * ITEM_INTS);
-    const int kind = rec[0], at = rec[1], c = rec[2], n = rec[3], last = rec[4], b = rec[5];
+    const int kind = rec[0], at = rec[1], c = rec[2], n = rec[3], last = rec[4], b = rec[5], chunk = rec[6];
     const scalar_i32 *pages = (const scalar_i32 *)(p.page_table + (int64_t)b * p.pages_per_seq);   // (the launch does not write it: scalar loads)
     if (kind == ITEM_OWN) {
       const Sight see(n, last);
       attend_item<HD, 4>(p, sm.fold, w.own, at, g, pages, see, c, w.own_runs, last == 0 && see.runs <= w.own_runs);
     } else {
-      attend_shared<HD>(p, sm, w.shared, pages, w.rows + at, last, g, c, c * w.shared_runs, min(n, (c + 1) * w.shared_runs));
+      attend_shared<HD>(p, sm, w.shared, pages, w.rows + at, last, g, c, c * chunk, min(n, (c + 1) * chunk));
     }
   }
 }
@@ -532,22 +557,28 @@ __global__ __launch_bounds__(256, 2) void attn_shared_kernel(RangeAttn p, Shared
 template <int NT>
 __global__ __launch_bounds__(NT) void shared_items_kernel(RangeAttn p, SharedPrompts q, SharedWork w) {
   constexpr int LENGTHS = 64;
-  __shared__ int count[LENGTHS], off[NT + 1], pre[NT + 1], claim[NT], s_ctx[NT], s_start[NT], first_item[NT], first_own[NT], cnt[NT], sh[NT], s_rows[NT];
-  const int t = threadIdx.x, listed0 = q.offsets[0], listed1 = q.offsets[q.n_groups];
+  __shared__ int count[LENGTHS], off[NT + 1], pre[NT + 1], claim[NT], s_ctx[NT], s_start[NT], first_item[NT], first_own[NT], cnt[NT], sh[NT], s_chunk[NT], s_chunks[NT], s_parts[NT], s_rows[NT];
+  const int t = threadIdx.x;
+  // (from places that are there for every thread: behind a condition each read would wait for the one before it)
+  const int shared0 = q.shared[min(t, q.n_groups - 1)], ctx0 = p.ctx_len[min(t, p.n_seq - 1)], off0 = q.offsets[min(t, q.n_groups)];
+  const int listed0 = q.offsets[0], listed1 = q.offsets[q.n_groups];
   const bool listed = listed0 >= 0 && t >= listed0 && listed1 <= p.n_seq && t < listed1;
   const int named = listed ? q.rows ? q.rows[t] : t : -1;   // (under way with everything else)
   int bad = 0;
   if (t < LENGTHS) count[t] = 0;
   for (int i = t; i <= q.n_groups; i += NT) {
-    off[i] = q.offsets[i];
+    off[i] = i == t ? off0 : q.offsets[i];
     bad |= off[i] < 0 || off[i] > p.n_seq;
   }
-  const int ctx = t < p.n_seq ? min(max(p.ctx_len[t], 0), p.max_ctx) : 0;
-  const int runs = t < q.n_groups ? min(max(q.shared[t], 0), q.max_shared) >> 5 : 0;
+  const int ctx = t < p.n_seq ? min(max(ctx0, 0), p.max_ctx) : 0;
+  const int runs = t < q.n_groups ? min(max(shared0, 0), q.max_shared) >> 5 : 0;
   s_ctx[t] = ctx;
   claim[t] = NT;
-  s_start[t] = 0;
+  s_start[t] = s_parts[t] = 0;
   sh[t] = runs;
+  int chunks = 0;
+  s_chunk[t] = runs ? w.cut.chunk(runs, chunks) : 0;
+  s_chunks[t] = chunks;
   __syncthreads();
   for (int i = t; i < q.n_groups; i += NT) bad |= off[i] > off[i + 1];
   bad = __syncthreads_or(bad);
@@ -570,17 +601,18 @@ __global__ __launch_bounds__(NT) void shared_items_kernel(RangeAttn p, SharedPro
   if (shares) {
     w.rows[place] = s_rows[place] = row;
     s_start[row] = sh[gr];
+    s_parts[row] = s_chunks[gr];
   }
   __syncthreads();
   const int own_runs = (ctx + 31) / 32 - s_start[t], own_chunks = (own_runs + w.own_runs - 1) / w.own_runs;
   const int mine = bad || t >= q.n_groups ? 0 : pre[off[t + 1]] - pre[off[t]];
   cnt[t] = mine;
-  const int tiles = (mine + w.tile_rows - 1) / w.tile_rows, chunks = (runs + w.shared_runs - 1) / w.shared_runs;
+  const int tiles = (mine + w.tile_rows - 1) / w.tile_rows;
   const int2 items = make_int2(tiles * chunks, max(0, own_chunks - 1));
   const int2 at = block_scan<NT>(items, &total);
   first_item[t] = at.x - items.x;
   first_own[t] = at.y - items.y;
-  if (t < p.n_seq) w.start[t] = s_start[t];
+  if (t < p.n_seq) w.start[t] = make_int2(s_start[t], s_parts[t]);
   // rows' last chunks, longest first (in no order among equals: who takes an item changes nothing in its result): places by counting
   const int last_runs = own_chunks > 0 ? own_runs - (own_chunks - 1) * w.own_runs : 0;   // 1 .. own_runs
   if (last_runs) atomicAdd(&count[LENGTHS - 1 - last_runs * (LENGTHS - 1) / w.own_runs], 1);
@@ -600,18 +632,18 @@ __global__ __launch_bounds__(NT) void shared_items_kernel(RangeAttn p, SharedPro
     }
     return lo;
   };
-  auto put = [&](int i, int kind, int a, int c, int n, int last, int b) {
+  auto put = [&](int i, int kind, int a, int c, int n, int last, int b, int chunk) {
     if (i >= w.cap) return;
     int4 *rec = (int4 *)(w.items + (int64_t)i * ITEM_INTS);
     rec[0] = make_int4(kind, a, c, n);
-    rec[1] = make_int4(last, b, 0, 0);
+    rec[1] = make_int4(last, b, chunk, 0);
   };
-  auto put_own = [&](int i, int b, int c, int ctx, int start) { put(i, ITEM_OWN, b, c, ctx, start, b); };
+  auto put_own = [&](int i, int b, int c, int ctx, int start) { put(i, ITEM_OWN, b, c, ctx, start, b, 0); };
   for (int i = t; i < total.x; i += NT) {
     const int k = find(first_item, q.n_groups, i), j = i - first_item[k];
     const int n_tiles = (cnt[k] + w.tile_rows - 1) / w.tile_rows, per = (cnt[k] + n_tiles - 1) / n_tiles, tile = j % n_tiles, c = j / n_tiles;   // tiles of one chunk side by side
     const int rows = pre[off[k]] + tile * per;
-    put(i, ITEM_SHARED, rows, c, sh[k], min(per, cnt[k] - tile * per), s_rows[rows]);
+    put(i, ITEM_SHARED, rows, c, sh[k], min(per, cnt[k] - tile * per), s_rows[rows], s_chunk[k]);
   }
   for (int i = t; i < total.y; i += NT) {
     const int b = find(first_own, p.n_seq, i);
@@ -622,7 +654,7 @@ __global__ __launch_bounds__(NT) void shared_items_kernel(RangeAttn p, SharedPro
 
 // Rows of several parts: a workgroup per (row, kv head), four elements of a head per thread, parts folded in order, eight loads under way (64 rows of 5 heads, 8 kv
 // heads, 20 parts: 8.2 us; by four times as many threads, the parts cut in four, 11.9; by the workgroup that ends last in the main kernel, the call 58 -> 146).
-struct MergeRows { Parts first, second; const int32_t *start; int32_t first_runs, second_runs, window, sinks; };
+struct MergeRows { Parts first, second; const int2 *start; int32_t second_runs, window, sinks; };
 template <int HD>
 __global__ __launch_bounds__(256) void attn_join_kernel(RangeAttn p, MergeRows q) {
   const int b = blockIdx.x / p.Hkv, g = blockIdx.x % p.Hkv, G = p.Hq / p.Hkv;
@@ -644,8 +676,9 @@ __global__ __launch_bounds__(256) void attn_join_kernel(RangeAttn p, MergeRows q
 #pragma unroll
     for (int u = 0; u < 8; ++u) load(q.first, u, min((int)threadIdx.x, G * (HD / 4) - 1), ml[u], o[u]);
   if (q.start) {
-    n1 = (q.start[b] + q.first_runs - 1) / q.first_runs;
-    n2 = ((ctx + 31) / 32 - q.start[b] + q.second_runs - 1) / q.second_runs;
+    const int2 at = q.start[b];
+    n1 = at.y;
+    n2 = ((ctx + 31) / 32 - at.x + q.second_runs - 1) / q.second_runs;
   } else {
     n2 = (Sight(ctx, q.window, q.sinks).runs + q.second_runs - 1) / q.second_runs;
   }
@@ -736,14 +769,18 @@ int64_t most_window_parts(int64_t pairs, int64_t runs) {
   return std::max(chunks > 1 ? std::min<int64_t>(1024, pairs * chunks) : 0, pairs > 256 && runs >= 48 ? 4 * std::min<int64_t>(pairs, 352) : 0);
 }
 
-// How a call with shared prompts is cut: by its shape alone, so that a row's result does not depend on what the other rows hold.  A row's own part
+// How a call with shared prompts is cut: by its shape, and a group's shared runs by their number, so that a row's result does not depend on what the other rows hold.  A row's own part
 // goes in chunks of up to 64 runs (16 prompts of 2048 with 16 rollouts each, 7B shape: chunks of 16, 32, 64 and 128 runs 165, 158, 155 and 155 us) and
 // at least 16 (32 rows of 4 prompts of 1000 and 300 on average, 7B shape: by 4, 8 and 16 runs 23.1, 21.6 and 20.8).  Shared runs are cut
-// into as many chunks as make 256 workgroups, or 512 where that leaves 24 runs each: every chunk leaves a part of every row.  Longer ones do
-// where the rows' own parts keep the chip busy meanwhile: half of their time, at a quarter of the most they could be and 0.9 us a run.  (Calls by 64, 256, 512
-// and 1024 workgroups, us: 64 rollouts of one prompt of 16384, 32B shape, 185, 61, 57, 71; 16 of them 60, 38, 49, 70; 16 prompts of 2048 with
-// 16 rollouts of 1500 on average each, 7B shape, 153, 169, 179, 192; 4 prompts of 4096 with 16 rollouts of 300 44, 36, 44, 44.)
-struct SharedSplit { Split own, shared; int tile_rows; int64_t cap; };
+// into as many chunks as make 256 workgroups, 384 where that leaves 24 runs each, 512 where that leaves 48: every chunk leaves a part of every row, and rows' own chunks wait for a place
+// behind them (64 rollouts of one prompt, 32B shape, us by workgroups: 448 runs, 240 51.0, 336 47.7, 384 49.0, 456 52.6; 512 runs, 264 52.3, 360 51.2, 384 52.0, 456 54.7; 1640
+// runs, 384 120, 512 115).  Longer ones do where the rows' own parts keep the chip busy meanwhile: half of their time, at a quarter of the most they could be and 0.9 us a run
+// (16 prompts of 2048 with 16 rollouts of 1500 on average each, 7B shape, by 64, 256 and 512 workgroups 153, 169 and 179; 4 prompts of 4096 with 16 rollouts of 300 44, 36, 44).
+// What own parts could be is a bound that may be far above what they are, in a captured step above all, so chunks are no longer than OWN_RUNS for it (the same 64 rollouts of up to 512 runs,
+// max_ctx 17584 54 us, 131072 64, without this limit 295; the 16 prompts 148 and 148).
+constexpr int64_t OWN_RUNS = 64;         // (by head dimension 128)
+constexpr int64_t SHARED_GROUPS = 512;   // most workgroups of shared runs that are cut
+struct SharedSplit { Split own; SharedCut cut; int chunks; int64_t shared_parts; int tile_rows; int64_t cap; };
 SharedSplit shared_split(int n_seq, int n_groups, int Hq, int Hkv, int hd, int max_ctx, int max_shared) {
   SharedSplit s;
   s.tile_rows = 128 / (Hq / Hkv);
@@ -753,35 +790,37 @@ SharedSplit shared_split(int n_seq, int n_groups, int Hq, int Hkv, int hd, int m
   const int64_t runs = std::max(1, max_shared / 32), units = n_groups * up(up(n_seq, n_groups), s.tile_rows) * Hkv;
   const int64_t own_bytes = (int64_t)n_seq * Hkv * (max_ctx - max_shared) * hd;   // (a quarter of four bytes per element and position)
   const int64_t own_runs = own_bytes / 5500000 * 128 / hd * 5 / 9;                // of 0.9 us (by head dimension) in half of their time at 5.5 TB/s
-  int64_t chunks = std::max<int64_t>(1, (runs * units >= 24 * 512 ? 512 : 256) / units);
-  while (chunks > 1 && chunks * chunks > 2 * runs) --chunks;   // (as for windows; 8 rollouts of one prompt of 16384, 7B shape, 33 -> 30 us)
-  s.shared.chunk = (int)std::min(up(runs, 4) * 4, std::max<int64_t>({8, own_runs, up(up(runs, chunks), 4) * 4}));
-  s.shared.chunk = (int)up(up(runs, up(runs, s.shared.chunk)), 4) * 4;   // (chunks of one length)
-  s.shared.chunks = (int)up(runs, s.shared.chunk);
-  s.shared.parts = (int64_t)n_seq * Hkv * s.shared.chunks;
-  s.cap = (n_groups + n_seq / s.tile_rows) * (int64_t)s.shared.chunks + (int64_t)n_seq * s.own.chunks;
+  int64_t most[3];
+  for (int i = 0; i < 3; ++i) {
+    most[i] = std::max<int64_t>(1, (i + 2) * SHARED_GROUPS / 4 / units);
+    s.cut.by[i] = Divisor((uint32_t)most[i]);
+  }
+  s.cut.from[0] = (int32_t)up(24 * 384, units);
+  s.cut.from[1] = (int32_t)up(48 * 512, units);
+  s.cut.own_runs = (int32_t)std::min<int64_t>(up(own_runs, 4) * 4, OWN_RUNS * 128 / hd);
+  s.chunks = (int)std::min(most[(runs >= s.cut.from[0]) + (runs >= s.cut.from[1])], up(runs, std::max(8, s.cut.own_runs)));   // the most of a group
+  s.shared_parts = (int64_t)n_seq * Hkv * s.chunks;
+  s.cap = (n_groups + n_seq / s.tile_rows) * (int64_t)s.chunks + (int64_t)n_seq * s.own.chunks;
   return s;
 }
 
 // The largest number of parts and items of any call of as many rows, groups and positions or fewer.  Own parts: chunks of less than 64 runs are taken where those of twice
-// the length would be less than 2048.  Shared parts: chunks squared stay below twice the runs, and they are 512 / units at most, or 1; units are a kv head's groups at least, and its tiles.
+// the length would be less than 2048.  Shared parts: chunks hold eight runs at least, and they are SHARED_GROUPS / units at most, or 1; units are a kv head's groups at least, and its tiles.
 struct SharedMost { int64_t own_parts, shared_parts, cap; };
 SharedMost most_shared(int n_seq, int n_groups, int Hq, int Hkv, int max_ctx, int max_shared) {
-  const int64_t pairs = (int64_t)n_seq * Hkv, tile_rows = 128 / (Hq / Hkv), runs = std::max(1, max_shared / 32);
-  int64_t chunks = 1;
-  while (chunks < 512 && (chunks + 1) * (chunks + 1) <= 2 * runs) ++chunks;
+  const int64_t pairs = (int64_t)n_seq * Hkv, tile_rows = 128 / (Hq / Hkv), chunks = std::clamp<int64_t>(up(max_shared / 32, 8), 1, SHARED_GROUPS);
   SharedMost m;
   m.own_parts = std::max(pairs * up(max_ctx, 64 * 32), std::min<int64_t>(4096, pairs * up(max_ctx, 16 * 32)));
-  m.shared_parts = std::min(pairs * chunks, std::max(pairs, 512 * tile_rows));
+  m.shared_parts = std::min(pairs * chunks, std::max(pairs, SHARED_GROUPS * tile_rows));
   const int64_t tiles = n_groups + n_seq / tile_rows;
-  m.cap = std::min(tiles * chunks, std::max<int64_t>(tiles, 1024 / Hkv)) + up(m.own_parts, Hkv);
+  m.cap = std::min(tiles * chunks, std::max<int64_t>(tiles, 2 * SHARED_GROUPS / Hkv)) + up(m.own_parts, Hkv);
   return m;
 }
 
 int64_t part_floats(int G, int hd) { return (int64_t)G * hd + ATTN_ML; }
-Parts take_parts(float *&at, const Split &s, int G, int hd) {
-  Parts r{at, at + s.parts * G * hd, s.chunks};
-  at += s.parts * part_floats(G, hd);
+Parts take_parts(float *&at, int64_t parts, int chunks, int G, int hd) {
+  Parts r{at, at + parts * G * hd, chunks};
+  at += parts * part_floats(G, hd);
   return r;
 }
 
@@ -798,21 +837,21 @@ int64_t window_workspace_bytes(int n_seq, int Hq, int Hkv, int hd, int max_ctx, 
 int launch_attention_window(const RangeAttn &p, int window, int sinks, void *workspace, hipStream_t s) {
   const Split sp = window_split(p.n_seq, p.Hkv, p.hd, p.max_ctx, window, sinks);
   float *at = (float *)workspace;
-  const Parts parts = take_parts(at, sp, p.Hq / p.Hkv, p.hd);
+  const Parts parts = take_parts(at, sp.parts, sp.chunks, p.Hq / p.Hkv, p.hd);
   with_head(p.hd, [&](auto HD) {
     constexpr int hd = decltype(HD)::value;
     const dim3 grid((unsigned)((int64_t)p.n_seq * sp.chunks * p.Hkv));
     if (sp.waves == 8) hipLaunchKernelGGL((attn_window_kernel<hd, 8>), grid, dim3(512), 0, s, p, parts, window, sinks, sp.chunk);
     else hipLaunchKernelGGL((attn_window_kernel<hd, 4>), grid, dim3(256), 0, s, p, parts, window, sinks, sp.chunk);
     if (sp.chunks > 1) {
-      const MergeRows q{parts, parts, nullptr, 1, sp.chunk, window, sinks};
+      const MergeRows q{parts, parts, nullptr, sp.chunk, window, sinks};
       hipLaunchKernelGGL((attn_join_kernel<hd>), dim3(p.n_seq * p.Hkv), dim3(256), 0, s, p, q);
     }
   });
   return ok();
 }
 
-static int64_t shared_ints(int n_seq, int64_t cap) { return (HEAD_INTS + cap * ITEM_INTS + 2 * n_seq + 63) / 64 * 64; }
+static int64_t shared_ints(int n_seq, int64_t cap) { return (HEAD_INTS + cap * ITEM_INTS + 3 * n_seq + 63) / 64 * 64; }
 
 // Calls in which every row reads all of its context by itself, in one or two launches instead of three.
 // They hold at most 512 MiB, and sharing would read at most 128 MiB less, which is what the list and the join cost (us, by the list / every row by itself: 32 rows of 4 prompts
@@ -837,13 +876,13 @@ int launch_attention_shared(const RangeAttn &p, const SharedPrompts &q, void *wo
   SharedWork w;
   w.head = (int32_t *)workspace;
   w.items = w.head + HEAD_INTS;
-  w.rows = w.items + sp.cap * ITEM_INTS;
-  w.start = w.rows + p.n_seq;
+  w.start = (int2 *)(w.items + sp.cap * ITEM_INTS);
+  w.rows = (int32_t *)(w.start + p.n_seq);
   float *at = (float *)(w.head + shared_ints(p.n_seq, sp.cap));
-  w.own = take_parts(at, sp.own, G, p.hd);
-  w.shared = take_parts(at, sp.shared, G, p.hd);
+  w.own = take_parts(at, sp.own.parts, sp.own.chunks, G, p.hd);
+  w.shared = take_parts(at, sp.shared_parts, sp.chunks, G, p.hd);
   w.own_runs = sp.own.chunk;
-  w.shared_runs = sp.shared.chunk;
+  w.cut = sp.cut;
   w.tile_rows = sp.tile_rows;
   w.cap = (int32_t)sp.cap;
   if (p.n_seq <= 256) hipLaunchKernelGGL(shared_items_kernel<256>, dim3(1), dim3(256), 0, s, p, q, w);
@@ -851,7 +890,7 @@ int launch_attention_shared(const RangeAttn &p, const SharedPrompts &q, void *wo
   with_head(p.hd, [&](auto HD) {
     constexpr int hd = decltype(HD)::value;
     hipLaunchKernelGGL((attn_shared_kernel<hd>), dim3((unsigned)std::min<int64_t>(sp.cap * p.Hkv, 4096)), dim3(256), 0, s, p, w);
-    const MergeRows m{w.shared, w.own, w.start, w.shared_runs, w.own_runs, 0, 0};
+    const MergeRows m{w.shared, w.own, w.start, w.own_runs, 0, 0};
     hipLaunchKernelGGL((attn_join_kernel<hd>), dim3(p.n_seq * p.Hkv), dim3(256), 0, s, p, m);
   });
   return ok();
