@@ -740,15 +740,17 @@ int64_t window_runs(int max_ctx, int window, int sinks) {
 // 129 -> 117; 352 pairs, 256 runs 264 -> 236; 384 pairs 150 / 149; 312 pairs, 40 runs 47 / 46).
 // 256 workgroups are enough where rows see equally much (32 pairs, 128 runs: 128 workgroups 19.5, 256 17.0, 512 18.4, 1024 23.4).  A window over whole contexts, of which
 // the longest may be several times the mean, has up to 1024, many of them with nothing to do (longest row / mean of lognormal lengths 4 to 5: 102 rows, one kv head of 32,
-// mean 1150, 21.5 -> 11.1; 20 rows, two of 128, mean 2000, 25.7 -> 17.5; but 16 rows of 4300 each, two of 128, 14.1 -> 16.1).
+// mean 1150, 21.5 -> 11.1; 20 rows, two of 128, mean 2000, 25.7 -> 17.5; but 16 rows of 4300 each, two of 128, 14.1 -> 16.1).  So has any window of 512 runs or more over up to 256
+// pairs, as rows may see little of it (lognormal lengths with a mean of 4000, window 32768, 7B shape: 16 rows 74 -> 44, 32 187 -> 88, 64 217 -> 171; rows of 33000 each 167 -> 173, 364 -> 333,
+// 638 -> 648); more pairs lose more than they gain (200 of 200, equal rows 264 -> 285).
 struct Split { int64_t parts; int chunk, chunks, waves; };
 Split window_split(int n_seq, int Hkv, int hd, int max_ctx, int window, int sinks) {
   const int64_t runs = window_runs(max_ctx, window, sinks), pairs = (int64_t)n_seq * Hkv;
   int64_t chunks = 1;
-  const bool whole = window >= max_ctx;
+  const bool whole = window >= max_ctx, unequal = whole || (runs >= 512 && pairs <= 256);
   const bool little = runs * hd <= 2560 || (pairs <= 8 && runs * std::max(hd, 64) <= 5120);
-  if ((pairs < 128 || whole) && !little) {
-    chunks = std::max<int64_t>(1, (whole ? 1024 : 256) / pairs);
+  if ((pairs < 128 || unequal) && !little) {
+    chunks = std::max<int64_t>(1, (unequal ? 1024 : 256) / pairs);
     while (chunks > 1 && chunks * chunks > (whole ? 1 : 2) * runs) --chunks;
   } else if (pairs > 256 && pairs <= 352 && runs >= 48) {
     chunks = 4;
