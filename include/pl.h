@@ -471,10 +471,13 @@ int pl_debug_gemm_int8_plan(int32_t M, int32_t N, int32_t K, int32_t *kernel, in
 /* Page tables and slots of a batch's new tokens, from lengths.  With P = page_tokens, row b of len[b] tokens becomes one of want[b]:
  *   want > len   pages [ceil(len / P), ceil(want / P)) of its row of page_table are taken from the free list (from its end backwards, rows in order)
  *   want < len   pages [max(ceil(want / P), first_owned[b]), ceil(len / P)) go back (behind the list's end, rows in order), before any are taken; their
- *                entries of page_table stay as they are.  want = 0 retires a sequence.
+ *                entries of page_table stay as they are.  want = 0 retires a sequence; otherwise the row keeps its first want tokens as they are.
+ * A row's new tokens are those behind the ones that it has, so a row whose sequence ends and that begins another takes two calls (one captured step may hold both): one in which
+ * its want is 0 and every other row's is its len, and the step's own with that call's ctx_out as len.
  *   len, want        device int32 [n_seq], 0 .. pages_per_seq * P
  *   first_owned      device int32 [n_seq], or NULL: 0.  A row's pages below it belong to others too (a prompt that several rows share) and are not
- *                    given back; a row grows behind them only.
+ *                    given back; a row grows behind them only.  The caller puts their ids into the row's part of page_table, and their tokens into len; they go back with
+ *                    a row whose first_owned is 0, which has to be the last that reads them.
  *   page_table       device int32 [n_seq, pages_per_seq], updated
  *   free_pages       device int32 [n_pages], updated: the first free_count[0] entries are the pages that are free
  *   free_count, free_count_out   device int32 [1], before and after
