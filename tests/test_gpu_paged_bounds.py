@@ -40,7 +40,7 @@ def _call(heads, prompts, rows, own, most, shared_most, seed=0):
 
 
 @pytest.mark.parametrize("heads,prompts,rows", [((40, 8, 128), [16384], 64), ((40, 8, 128), [9000], 16), ((28, 4, 128), [2048, 4096, 700, 1000], 16), ((8, 1, 64), [30000, 64], 20),
-                                                ((16, 4, 32), [6000] * 3, 3)])
+                                                ((16, 4, 32), [6000] * 3, 3), ((16, 1, 128), [45000], 512)])   # (the last: chunks of more pages than a wavefront has lanes)
 def test_bits_do_not_depend_on_the_bound_of_prompts(heads, prompts, rows):
     n = len(prompts) * rows
     least = max(max(prompts) + 200, (512 << 20) // (n * heads[1] * heads[2] * 4) + 1)   # (a call that shares)
