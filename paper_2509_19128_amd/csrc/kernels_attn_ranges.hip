@@ -45,7 +45,7 @@ struct SharedCut {
     c = min(max(c, max(8, own_runs)), up4(runs));
     chunks = (int)((float)runs * __builtin_amdgcn_rcpf((float)c));
     chunks += chunks * (int64_t)c < runs ? 1 : (chunks - 1) * (int64_t)c >= runs ? -1 : 0;
-    const int same = up4((int)((float)runs * __builtin_amdgcn_rcpf((float)chunks)) + 1);   // chunks of one length
+    const int same = up4((int)((float)runs * __builtin_amdgcn_rcpf((float)chunks) + 0.99f));   // chunks of one length
     return same < c && (int64_t)same * chunks >= runs ? same : c;
   }
 };
