@@ -544,8 +544,8 @@ int pl_attention_window(const void *q, const void *kv_pages, const int32_t *page
  *   shared_len     device int32 [n_groups], at most max_shared: positions [0, shared_len[k]) hold the same in every row of group k, in the row's own pages or in
  *                  pages that rows have in common.  Whole runs of 32 of them are read through the page table of one of the rows, the rest through each row's own; a row whose
  *                  context is shorter than those runs attends by itself.
- * max_ctx and max_shared may be far above what rows hold, as in a captured step: shared positions are cut by their own number (max_ctx - max_shared says how long the rest
- * could be, and costs up to a fifth where it is much less; the workspace grows with both).
+ * max_ctx and max_shared may be far above what rows hold, as in a captured step: shared positions are cut by their own number.  (max_ctx - max_shared says how long the rest
+ * could be, which is waited for meanwhile: far above what it is, it can cost a call of 30 us 20 more.  The workspace grows with both.)
  * Offsets that do not ascend or leave [0, n_seq] make no groups.  The result is the softmax over the whole context, as if nothing were shared; a row's bits depend
  * on n_seq, n_groups, max_ctx, max_shared, its group's shared_len, how many rows share it and its place among them, not on what the other rows hold.
  * workspace: pl_attention_shared_workspace_bytes bytes (which do for fewer rows and groups, a smaller max_ctx and a smaller max_shared too), nothing of value in it

@@ -529,8 +529,8 @@ __device__ __forceinline__ void attend_shared(const RangeAttn &p, Lds<HD> &lds, 
 
 // A workgroup an item, and more where there are more than 4096 (workgroups without one cost nothing: 512 to 100000 the same time; 512 that draw items from a counter
 // take 6 to 10 us longer).
-// 16 prompts of 2048 with 16 rollouts of 1500 on average each, 7B shape, 779 MB and 11.5 GFLOP: 137 us, 5.7 TB/s.  64 rollouts of one prompt of 16384, 32B shape, 109 MB
-// and 18.9 GFLOP: 44 us, bound by the matrix products and the vector operations on their results.
+// 16 prompts of 2048 with 16 rollouts of 1500 on average each, 7B shape, 779 MB and 11.5 GFLOP: 138 to 154 us, 5.1 to 5.7 TB/s.  64 rollouts of one prompt of up to 16384, 32B shape, 109 MB
+// and 18.9 GFLOP: 42 us, bound by the matrix products and the vector operations on their results.
 template <int HD>
 __global__ __launch_bounds__(256, 2) void attn_shared_kernel(RangeAttn p, SharedWork w) {
   __shared__ __attribute__((aligned(16))) Lds<HD> sm;
@@ -779,7 +779,7 @@ int64_t most_window_parts(int64_t pairs, int64_t runs) {
 // runs, 384 120, 512 115).  Longer ones do where the rows' own parts keep the chip busy meanwhile: half of their time, at a quarter of the most they could be and 0.9 us a run
 // (16 prompts of 2048 with 16 rollouts of 1500 on average each, 7B shape, by 64, 256 and 512 workgroups 153, 169 and 179; 4 prompts of 4096 with 16 rollouts of 300 44, 36, 44).
 // What own parts could be is a bound that may be far above what they are, in a captured step above all, so chunks are no longer than OWN_RUNS for it (the same 64 rollouts of up to 512 runs,
-// max_ctx 17584 54 us, 131072 64, without this limit 295; the 16 prompts 148 and 148).
+// max_ctx 17584 54 us, 131072 64, without this limit 295; the 4 prompts 31, 54 and 87; the 16 prompts 148, 148 and 148, with a limit of 48 or 32 153 and 156).
 constexpr int64_t OWN_RUNS = 64;         // (by head dimension 128)
 constexpr int64_t SHARED_GROUPS = 512;   // most workgroups of shared runs that are cut
 struct SharedSplit { Split own; SharedCut cut; int chunks; int64_t shared_parts; int tile_rows; int64_t cap; };
